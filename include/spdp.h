@@ -255,6 +255,174 @@ int spdp_spmspv_many_mask(const spdp_handle_t* handles, int32_t count,
 int spdp_spmm(spdp_handle_t h, const uint16_t* X, int64_t n_tokens,
               uint16_t* Y, void* stream);
 
+/*
+ * spdp_spmm_grad -- the gradient of spdp_spmm with respect to its input:
+ * dX = dY W_sp for n_tokens tokens, on the same encoded matrix (nothing dense
+ * or transposed is kept), on the matrix cores, fp32 accumulation, one rounding
+ * to fp16 (nearest even).
+ *
+ *   h          as for spdp_spmm (tile_m = 256, tile_k >= 16, fp16 Values;
+ *              other handles: SPDP_ERR_UNSUPPORTED).
+ *   dY         device, n_tokens x rows fp16, row-major, 16-byte aligned. An
+ *              infinity or NaN in a token's dY may make every entry of the
+ *              token's dX NaN (it meets the pruned zeros).
+ *   n_tokens   1 <= n_tokens <= 65535 * 32.
+ *   dX         device, n_tokens x cols fp16, row-major, 16-byte aligned, fully
+ *              overwritten; must not overlap dY.
+ *   workspace  device, 256-byte aligned, spdp_spmm_grad_workspace bytes (which
+ *              may be 0: then NULL will do), the call's alone until the stream
+ *              has passed it.
+ *   stream     hipStream_t to enqueue on.
+ *
+ * Asynchronous; allocates nothing and keeps nothing, so that it may be
+ * captured, and calls on one handle may overlap on different streams, each with
+ * a workspace of its own. Where the grid leaves compute units idle the stripes
+ * are split into ranges, whose fp32 sums a second kernel adds in order: the
+ * summation order depends on the matrix, the token count and the device's
+ * compute-unit count alone (and on the tuning variables SPDP_GRAD_TOKENS and
+ * SPDP_GRAD_SPLITS, when set).
+ */
+int spdp_spmm_grad_workspace(spdp_handle_t h, int64_t n_tokens, size_t* bytes);
+int spdp_spmm_grad(spdp_handle_t h, const uint16_t* dY, int64_t n_tokens,
+                   uint16_t* dX, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection: a bank holds,
+ * for one projection (rows x cols), `count` adapters of rank `rank`, and token
+ * t of a call has the adapter ids[t]:
+ *     h[t] = A[ids[t]] x[t]
+ *     Y[t] = fp16(base[t] + scale[ids[t]] * (B[ids[t]] h[t]))
+ * where base is what the shared projection gave (spdp_spmspv*, spdp_spmm).
+ * Sums are fp32, and so is h between the two products. Where h meets B it is
+ * split into two fp16 numbers, together exact to 2^-22 of it or to 2^-37 of the
+ * token's largest |h|.
+ */
+typedef struct spdp_adapters {
+  const uint16_t* a;   /* device, count x rank x cols fp16 */
+  const uint16_t* b;   /* device, count x rank x rows fp16: B rank by rank */
+  const float* scale;  /* device, count */
+  int64_t rows, cols;  /* each at most 2^24 */
+  int32_t count;       /* 1 <= count <= 2048 */
+  int32_t rank;        /* 1 <= rank <= 128 */
+} spdp_adapters_t;
+
+/*
+ * spdp_adapt -- adds the adapters of n_banks projections (q, k and v; gate and
+ * up) in one call. No handle: the arrays are the caller's, and may be changed
+ * between calls.
+ *
+ *   banks      1 <= n_banks <= 8, all of one rank and one count.
+ *   X, base, Y n_banks device pointers each (X[i]: n_tokens x cols_i, base[i]
+ *              and Y[i]: n_tokens x rows_i, fp16, row-major). Any alignment
+ *              that fp16 has. X may be shared. Y[i] may be base[i]; else an
+ *              output overlaps no input and no other output.
+ *   ids        device, n_tokens; an id outside [0, count) is no adapter, and
+ *              the token's Y is its base. NULL: adapter 0 for every token.
+ *   H          NULL, or n_banks device pointers (n_tokens x rank fp32 each)
+ *              that receive h (0 for tokens without an adapter), which
+ *              spdp_adapt_grad reads.
+ *   n_tokens   1 <= n_tokens <= 2^20.
+ *   workspace  device, 256-byte aligned, spdp_adapt_workspace bytes, the call's
+ *              alone until the stream has passed it; it overlaps no other array.
+ *   stream     hipStream_t to enqueue on (of the current device, which all
+ *              arrays are on).
+ *
+ * Asynchronous; allocates nothing, keeps nothing, may be captured. The order of
+ * the sums depends on the sizes, the token's place among the tokens (where ids
+ * are given: none) and the device's compute-unit count; equal inputs give equal
+ * bits.
+ */
+int spdp_adapt_workspace(const spdp_adapters_t* banks, int32_t n_banks,
+                         int64_t n_tokens, int32_t with_ids, size_t* bytes);
+int spdp_adapt(const spdp_adapters_t* banks, int32_t n_banks,
+               const uint16_t* const* X, const int32_t* ids,
+               const uint16_t* const* base, uint16_t* const* Y, float* const* H,
+               int64_t n_tokens, void* workspace, size_t workspace_bytes,
+               void* stream);
+
+/*
+ * spdp_adapt_grad -- the gradients of one bank's spdp_adapt for dY, the
+ * gradient with respect to Y. With u[t] = B[ids[t]]^T dY[t]:
+ *     dX[t] = fp16(base[t] + scale[ids[t]] * (A[ids[t]]^T u[t]))
+ *     dA[i] = scale[i] * sum over the tokens of adapter i of u[t] x[t]^T
+ *     dB[i] = scale[i] * sum over the tokens of adapter i of h[t] dY[t]^T
+ * base is the shared projection's gradient with respect to its input
+ * (spdp_spmm_grad); that with respect to the base of Y is dY itself.
+ *
+ *   X, ids     the forward call's; H what it kept.
+ *   dY         device, n_tokens x rows fp16.
+ *   base, dX   device, n_tokens x cols fp16; dX may be base.
+ *   dA, dB     device, fp32, laid out as a and b, fully overwritten (adapters
+ *              without tokens: 0).
+ *   workspace  spdp_adapt_grad_workspace bytes; the rest as for spdp_adapt.
+ *
+ * The sums over an adapter's tokens run in a fixed order: equal inputs give
+ * equal bits.
+ */
+int spdp_adapt_grad_workspace(const spdp_adapters_t* bank, int64_t n_tokens,
+                              int32_t with_ids, size_t* bytes);
+int spdp_adapt_grad(const spdp_adapters_t* bank, const uint16_t* X,
+                    const int32_t* ids, const float* H, const uint16_t* dY,
+                    const uint16_t* base, uint16_t* dX, float* dA, float* dB,
+                    int64_t n_tokens, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * Norm and position rotation of the heads of queries and keys, one pass over
+ * what the projections wrote. For every token and head v of `dim` numbers:
+ * n = v / sqrt(mean(v^2) + eps) * weight (weight NULL: n = v), and then each
+ * pair (p, q) of the leading `rot` numbers of n becomes
+ *     (p cos - q sin, q cos + p sin)
+ * with the angles of the token's position; the rest stay as they are. fp32
+ * arithmetic, one rounding to fp16.
+ */
+typedef struct spdp_rotation {
+  const int32_t* positions; /* device, n_tokens; one outside [0, table) is a
+                               padding token, whose outputs are left as they
+                               were (backward: its dx is 0) */
+  const float* cosine;      /* device, table x rot/2 */
+  const float* sine;        /* device, table x rot/2 */
+  int64_t table;            /* 1 <= table <= 2^30 */
+  int32_t dim;              /* of a head: even, at most 512 */
+  int32_t rot;              /* even, 2 <= rot <= dim */
+  int32_t interleaved;      /* 0: pair i is (i, i + rot/2); else (2i, 2i + 1) */
+  float eps;                /* >= 0 */
+} spdp_rotation_t;
+
+typedef struct spdp_heads {
+  const uint16_t* x;      /* device, n_tokens x heads x dim fp16 */
+  const uint16_t* weight; /* device, dim fp16, or NULL: no norm */
+  const uint16_t* dy;     /* backward only: as x */
+  uint16_t* y;            /* output, as x: the heads, or backward dx */
+  float* dweight;         /* backward only: dim fp32, where there is a weight */
+  int32_t heads;          /* 1 <= heads <= 65536 */
+} spdp_heads_t;
+
+/*
+ * spdp_rotate_heads -- the forward pass for 1 to 8 inputs (queries, keys) of
+ * the same tokens, in one launch. 1 <= n_tokens <= 2^24. y may be its own x as
+ * a whole (in place), and overlaps no other array. Any alignment that the types
+ * have. Asynchronous; allocates nothing, keeps nothing, may be captured.
+ *
+ * spdp_rotate_heads_grad -- the gradients: y receives that with respect to x
+ * (it may be its own x or dy as a whole), dweight that with respect to weight
+ * (the sum over tokens and heads, in a fixed order). `workspace` is device
+ * memory, 256-byte aligned, of spdp_rotate_heads_grad_workspace bytes (0
+ * without weights), the call's alone until the stream has passed it.
+ */
+int spdp_rotate_heads(const spdp_heads_t* inputs, int32_t n_inputs,
+                      const spdp_rotation_t* rotation, int64_t n_tokens,
+                      void* stream);
+int spdp_rotate_heads_grad_workspace(const spdp_heads_t* inputs,
+                                     int32_t n_inputs,
+                                     const spdp_rotation_t* rotation,
+                                     int64_t n_tokens, size_t* bytes);
+int spdp_rotate_heads_grad(const spdp_heads_t* inputs, int32_t n_inputs,
+                           const spdp_rotation_t* rotation, int64_t n_tokens,
+                           void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* spdp_reserve -- size the handle's workspace for batches up to max_batch. */
 int spdp_reserve(spdp_handle_t h, int32_t max_batch);
 

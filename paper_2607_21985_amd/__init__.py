@@ -31,6 +31,10 @@ __all__ = [
     "encode_rtn",
     "encode_rtn_host",
     "spmspv_many",
+    "Adapters",
+    "adapters_many",
+    "rotate_heads",
+    "rotate_heads_grad",
     "MASKS",
     "Chain",
     "prune_magnitude",
@@ -48,6 +52,9 @@ EXPORTED_SYMBOLS = (
     "spdp_format", "spdp_prune_magnitude", "spdp_calibrate_threshold",
     "spdp_threshold_code", "spdp_strerror", "spdp_last_error",
     "spdp_encode_rtn", "spdp_encode_rtn_host", "spdp_spmspv_noalloc", "spdp_spmm",
+    "spdp_spmm_grad_workspace", "spdp_spmm_grad", "spdp_adapt_workspace", "spdp_adapt",
+    "spdp_adapt_grad_workspace", "spdp_adapt_grad",
+    "spdp_rotate_heads", "spdp_rotate_heads_grad_workspace", "spdp_rotate_heads_grad",
 )
 
 SPDP_OK = 0
@@ -83,6 +90,23 @@ class _Format(ctypes.Structure):
     ]
 
 
+class _Bank(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("count", ctypes.c_int32), ("rank", ctypes.c_int32)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("cosine", ctypes.c_void_p), ("sine", ctypes.c_void_p),
+                ("table", ctypes.c_int64), ("dim", ctypes.c_int32), ("rot", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("dy", ctypes.c_void_p),
+                ("y", ctypes.c_void_p), ("dweight", ctypes.c_void_p), ("heads", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -114,6 +138,16 @@ def lib() -> ctypes.CDLL:
     L.spdp_spmspv_many_mask.argtypes = [ctypes.POINTER(H), i32, ctypes.POINTER(ctypes.c_void_p), i32,
                                         ctypes.POINTER(ctypes.c_float), i32, ctypes.POINTER(ctypes.c_void_p),
                                         ctypes.c_void_p]
+    P, size = ctypes.c_void_p, ctypes.c_size_t
+    L.spdp_spmm_grad_workspace.argtypes = [H, i64, ctypes.POINTER(size)]
+    L.spdp_spmm_grad.argtypes = [H, P, i64, P, P, size, P]
+    L.spdp_adapt_workspace.argtypes = [P, i32, i64, i32, ctypes.POINTER(size)]
+    L.spdp_adapt.argtypes = [P, i32, P, P, P, P, P, i64, P, size, P]
+    L.spdp_adapt_grad_workspace.argtypes = [P, i64, i32, ctypes.POINTER(size)]
+    L.spdp_adapt_grad.argtypes = [P, P, P, P, P, P, P, P, P, i64, P, size, P]
+    L.spdp_rotate_heads.argtypes = [P, i32, P, i64, P]
+    L.spdp_rotate_heads_grad_workspace.argtypes = [P, i32, P, i64, ctypes.POINTER(size)]
+    L.spdp_rotate_heads_grad.argtypes = [P, i32, P, i64, P, size, P]
     L.spdp_reserve.argtypes = [H, i32]
     L.spdp_split_plan.argtypes = [H, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]
     L.spdp_free.argtypes = [H]
@@ -129,6 +163,9 @@ def lib() -> ctypes.CDLL:
     for name in ("spdp_encode", "spdp_encode_host", "spdp_spmspv", "spdp_spmspv_noalloc", "spdp_spmm",
                  "spdp_spmspv_many",
                  "spdp_spmspv_many_mask",
+                 "spdp_spmm_grad_workspace", "spdp_spmm_grad", "spdp_adapt_workspace", "spdp_adapt",
+                 "spdp_adapt_grad_workspace", "spdp_adapt_grad",
+                 "spdp_rotate_heads", "spdp_rotate_heads_grad_workspace", "spdp_rotate_heads_grad",
                  "spdp_reserve", "spdp_split_plan",
                  "spdp_format",
                  "spdp_prune_magnitude", "spdp_calibrate_threshold", "spdp_threshold_code"):
@@ -153,6 +190,39 @@ def _u16(a: np.ndarray) -> np.ndarray:
 
 def _ptr(a: np.ndarray) -> ctypes.c_void_p:
     return ctypes.c_void_p(a.ctypes.data)
+
+
+def _tensor(t, name: str, dtype, shape) -> None:
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor")
+
+
+def _stream(stream, *tensors):
+    """The HIP stream to enqueue on, after a check of the tensors' device."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors:
+        if not t.is_cuda or t.device != dev:
+            raise ValueError("all tensors must be on one GPU")
+    if torch.cuda.current_device() != dev.index:
+        raise ValueError("the tensors are not on the current device")
+    s = stream if stream is not None else torch.cuda.current_stream(dev)
+    if s.device != dev:
+        raise ValueError("the stream is not on the tensors' device")
+    return s.cuda_stream
+
+
+def _workspace(size: int, device, stream):
+    """Device memory for one call. It belongs to the call's stream (or to the
+    graph that the stream is captured into), so that torch hands it out again
+    only to work behind the call."""
+    import torch
+    if stream is None:
+        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
 
 
 class Matrix:
@@ -284,6 +354,26 @@ class Matrix:
         self.spmm_into(x, y, stream)
         return y
 
+    def spmm_grad_into(self, dy, dx, stream=None) -> None:
+        """Enqueue the gradient of ``spmm`` with respect to its input,
+        ``dx = dy W_sp``, for ``dy`` [tokens, rows] into ``dx`` [tokens, cols]."""
+        import torch
+        n = dy.shape[0]
+        _tensor(dy, "dy", torch.float16, (n, self.rows))
+        _tensor(dx, "dx", torch.float16, (n, self.cols))
+        s = _stream(stream, dy, dx)
+        need = ctypes.c_size_t()
+        _check(lib().spdp_spmm_grad_workspace(self._h, n, ctypes.byref(need)))
+        ws = _workspace(need.value, dy.device, stream)
+        _check(lib().spdp_spmm_grad(self._h, dy.data_ptr(), n, dx.data_ptr(), ws.data_ptr(), need.value, s))
+
+    def spmm_grad(self, dy, stream=None):
+        """The gradient ``dy W_sp`` as a new fp16 tensor."""
+        import torch
+        dx = torch.empty((dy.shape[0], self.cols), dtype=torch.float16, device=dy.device)
+        self.spmm_grad_into(dy, dx, stream)
+        return dx
+
     def __call__(self, x, threshold: float, stream=None, mask: str = "token"):
         import torch
         y = torch.empty((x.shape[0], self.rows), dtype=torch.float16, device=x.device)
@@ -386,6 +476,181 @@ def spmspv_many(mats, xs, thresholds, ys, stream=None, mask: str = "token") -> N
                                        ctypes.c_void_p(s.cuda_stream)))
 
 
+class Adapters:
+    """The low-rank adapters of one projection (rows x cols), of one rank.
+
+    ``a`` is fp16 [count, rank, cols], ``b`` fp16 [count, rank, rows] (the
+    second factor rank by rank), ``scale`` fp32 [count], all contiguous on one
+    GPU. Nothing is copied: weights that are changed in place count from the
+    next call on.
+
+        y = fp16(base + scale[id] * (x a[id]^T) b[id])
+
+    with the adapter ``id`` of each token. ``base`` is the shared projection's
+    output (``Matrix``, ``spmspv_many``, ``Matrix.spmm``).
+    """
+
+    def __init__(self, a, b, scale):
+        import torch
+        if a.dim() != 3 or b.dim() != 3:
+            raise ValueError("a and b must be [count, rank, features]")
+        count, rank, cols = a.shape
+        _tensor(a, "a", torch.float16, (count, rank, cols))
+        _tensor(b, "b", torch.float16, (count, rank, b.shape[2]))
+        _tensor(scale, "scale", torch.float32, (count,))
+        _stream(None, a, b, scale)
+        self.a, self.b, self.scale = a, b, scale
+        self.count, self.rank, self.rows, self.cols = count, rank, b.shape[2], cols
+        self._bank = _Bank(a.data_ptr(), b.data_ptr(), scale.data_ptr(), self.rows, cols, count, rank)
+        need = ctypes.c_size_t()  # checks the sizes
+        _check(lib().spdp_adapt_workspace(ctypes.byref(self._bank), 1, 1, 0, ctypes.byref(need)))
+
+    def add_into(self, x, ids, base, y, h=None, stream=None) -> None:
+        """Enqueue ``y = base + the adapters' products of x`` for ``x`` [tokens,
+        cols], ``base`` and ``y`` [tokens, rows], fp16 (``y`` may be ``base``).
+
+        ``ids``: int32 [tokens], each token's adapter, one outside [0, count)
+        for none; or None, adapter 0 for all. ``h``: fp32 [tokens, rank] that
+        receives ``x a[id]^T``, which ``grad_into`` reads."""
+        adapters_many([self], [x], ids, [base], [y], None if h is None else [h], stream)
+
+    def __call__(self, x, ids, base, stream=None):
+        """``add_into`` a new tensor."""
+        import torch
+        y = torch.empty_like(base)
+        self.add_into(x, ids, base, y, stream=stream)
+        return y
+
+    def grad_into(self, x, ids, h, dy, base, dx, da, db, stream=None) -> None:
+        """Enqueue the gradients for ``dy`` [tokens, rows] of ``add_into``'s
+        ``y``: ``dx = base + the adapters' part`` fp16 [tokens, cols] (``base``:
+        the shared projection's gradient, ``Matrix.spmm_grad``; ``dx`` may be
+        ``base``), ``da`` and ``db`` fp32 like ``a`` and ``b`` (overwritten).
+        ``x``, ``ids`` and ``h`` are the forward call's."""
+        import torch
+        n = x.shape[0]
+        _tensor(x, "x", torch.float16, (n, self.cols))
+        _tensor(h, "h", torch.float32, (n, self.rank))
+        _tensor(dy, "dy", torch.float16, (n, self.rows))
+        _tensor(base, "base", torch.float16, (n, self.cols))
+        _tensor(dx, "dx", torch.float16, (n, self.cols))
+        _tensor(da, "da", torch.float32, self.a.shape)
+        _tensor(db, "db", torch.float32, self.b.shape)
+        some = (x, h, dy, base, dx, da, db, self.a)
+        if ids is not None:
+            _tensor(ids, "ids", torch.int32, (n,))
+            some += (ids,)
+        s = _stream(stream, *some)
+        need = ctypes.c_size_t()
+        bank = ctypes.byref(self._bank)
+        _check(lib().spdp_adapt_grad_workspace(bank, n, ids is not None, ctypes.byref(need)))
+        ws = _workspace(need.value, x.device, stream)
+        _check(lib().spdp_adapt_grad(bank, x.data_ptr(), None if ids is None else ids.data_ptr(), h.data_ptr(),
+                                     dy.data_ptr(), base.data_ptr(), dx.data_ptr(), da.data_ptr(), db.data_ptr(), n,
+                                     ws.data_ptr(), need.value, s))
+
+
+def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
+    """Enqueue ``Adapters.add_into`` of several projections (q, k and v; gate
+    and up) as one call. The banks have one rank and one count; ``ids`` goes for
+    all. Inputs may be shared."""
+    import torch
+    k = len(banks)
+    if not (len(xs) == len(bases) == len(ys) == k) or (hs is not None and len(hs) != k) or k == 0:
+        raise ValueError("banks, xs, bases, ys and hs must have one entry per projection")
+    n = xs[0].shape[0]
+    some = []
+    for i, (m, x, base, y) in enumerate(zip(banks, xs, bases, ys)):
+        _tensor(x, "x", torch.float16, (n, m.cols))
+        _tensor(base, "base", torch.float16, (n, m.rows))
+        _tensor(y, "y", torch.float16, (n, m.rows))
+        some += (x, base, y, m.a)
+        if hs is not None:
+            _tensor(hs[i], "h", torch.float32, (n, m.rank))
+            some.append(hs[i])
+    if ids is not None:
+        _tensor(ids, "ids", torch.int32, (n,))
+        some.append(ids)
+    s = _stream(stream, *some)
+    P = ctypes.c_void_p * k
+    bk = (_Bank * k)(*[m._bank for m in banks])
+    need = ctypes.c_size_t()
+    _check(lib().spdp_adapt_workspace(bk, k, n, ids is not None, ctypes.byref(need)))
+    ws = _workspace(need.value, xs[0].device, stream)
+    _check(lib().spdp_adapt(bk, k, P(*[x.data_ptr() for x in xs]), None if ids is None else ids.data_ptr(),
+                            P(*[b.data_ptr() for b in bases]), P(*[y.data_ptr() for y in ys]),
+                            None if hs is None else P(*[h.data_ptr() for h in hs]), n, ws.data_ptr(), need.value, s))
+
+
+def _heads(xs, dim, pos, cos, sin, ys, weights, eps, interleaved, stream, dys=None, dweights=None):
+    import torch
+    k = len(xs)
+    if k == 0 or len(ys) != k or any(v is not None and len(v) != k for v in (weights, dys, dweights)):
+        raise ValueError("every list must have one entry per input")
+    if dim < 1:
+        raise ValueError("dim must be at least 1")
+    n = xs[0].shape[0]
+    _tensor(pos, "pos", torch.int32, (n,))
+    if cos.dim() != 2:
+        raise ValueError("cos and sin must be [positions, rot / 2]")
+    _tensor(cos, "cos", torch.float32, cos.shape)
+    _tensor(sin, "sin", torch.float32, cos.shape)
+    some = [xs[0], pos, cos, sin]
+    inputs = (_Heads * k)()
+    for i, (x, y) in enumerate(zip(xs, ys)):
+        if x.dim() != 2 or x.shape[1] % dim or x.shape[1] == 0:
+            raise ValueError(f"x must be [tokens, heads * {dim}]")
+        _tensor(x, "x", torch.float16, (n, x.shape[1]))
+        _tensor(y, "the output", torch.float16, x.shape)
+        some += (x, y)
+        m = inputs[i]
+        m.x, m.y, m.heads = x.data_ptr(), y.data_ptr(), x.shape[1] // dim
+        w = None if weights is None else weights[i]
+        if w is not None:
+            _tensor(w, "a weight", torch.float16, (dim,))
+            some.append(w)
+            m.weight = w.data_ptr()
+        if dys is not None:
+            _tensor(dys[i], "dy", torch.float16, x.shape)
+            some.append(dys[i])
+            m.dy = dys[i].data_ptr()
+        d = None if dweights is None else dweights[i]
+        if d is not None:
+            _tensor(d, "a weight's gradient", torch.float32, (dim,))
+            some.append(d)
+            m.dweight = d.data_ptr()
+    s = _stream(stream, *some)
+    r = _Rotation(pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), cos.shape[0], dim, 2 * cos.shape[1],
+                  int(bool(interleaved)), eps)
+    return inputs, k, ctypes.byref(r), n, s
+
+
+def rotate_heads(xs, dim, pos, cos, sin, ys, weights=None, eps=1e-6, interleaved=False, stream=None) -> None:
+    """Enqueue the norm and position rotation of the heads of ``xs`` (queries,
+    keys; fp16 [tokens, heads * dim] as the projections write them) into ``ys``
+    (which may be ``xs``), one launch.
+
+    ``pos``: int32 [tokens], rows of ``cos`` and ``sin``, fp32 [positions,
+    rot / 2]; a token whose position is none of them is padding, and its outputs
+    are left as they were. ``weights``: per input the norm's fp16 [dim] weight,
+    or None for no norm. ``interleaved``: pairs are neighbours, else (i, i +
+    rot / 2)."""
+    inputs, k, r, n, s = _heads(xs, dim, pos, cos, sin, ys, weights, eps, interleaved, stream)
+    _check(lib().spdp_rotate_heads(inputs, k, r, n, s))
+
+
+def rotate_heads_grad(xs, dim, pos, cos, sin, dys, dxs, weights=None, dweights=None, eps=1e-6, interleaved=False,
+                      stream=None) -> None:
+    """Enqueue ``rotate_heads``'s gradients for ``dys``: ``dxs`` (0 for padding;
+    each may be its x or dy) and, for inputs with a weight, ``dweights`` (fp32
+    [dim], overwritten)."""
+    inputs, k, r, n, s = _heads(xs, dim, pos, cos, sin, dxs, weights, eps, interleaved, stream, dys, dweights)
+    need = ctypes.c_size_t()
+    _check(lib().spdp_rotate_heads_grad_workspace(inputs, k, r, n, ctypes.byref(need)))
+    ws = _workspace(need.value, xs[0].device, stream)
+    _check(lib().spdp_rotate_heads_grad(inputs, k, r, n, ws.data_ptr(), need.value, s))
+
+
 def encode_rtn(w: np.ndarray, tile=(256, 16), bits: int = 4) -> Matrix:
     """Quantize a pruned fp16 matrix to ``bits``-bit round-to-nearest codes
     (one scale per row), encode it with one byte per code and upload it."""
@@ -449,7 +714,9 @@ class Chain:
 
     ``add`` records one launch: a list of products that read one input
     (q, k and v; gate and up) goes out as one grouped launch, a single
-    product as a plain call. ``capture`` sizes every matrix's workspace for
+    product as a plain call. ``add_adapters`` and ``add_heads`` record what
+    stands between them: the requests' adapters, and the norm and rotation of
+    the heads. ``capture`` sizes every matrix's workspace for
     the batches recorded, issues the launches once eagerly and records them
     into a graph on a side stream; ``replay`` re-issues the whole chain on
     the current stream with one host call. Between replays the caller
@@ -471,9 +738,29 @@ class Chain:
         self._calls.append((list(mats), list(xs), [float(t) for t in thresholds], list(ys), mask))
         return self
 
+    def add_adapters(self, banks, xs, ids, bases, ys) -> "Chain":
+        """Record an ``adapters_many`` call, behind the launch that wrote ``bases``."""
+        if self._graph is not None:
+            raise RuntimeError("the chain is captured already")
+        if isinstance(banks, Adapters):
+            banks, xs, bases, ys = [banks], [xs], [bases], [ys]
+        args = (list(banks), list(xs), ids, list(bases), list(ys))
+        self._calls.append((None, args[1], None, lambda: adapters_many(*args), None))
+        return self
+
+    def add_heads(self, xs, dim, pos, cos, sin, ys, weights=None, eps=1e-6, interleaved=False) -> "Chain":
+        """Record a ``rotate_heads`` call, behind the launch that wrote ``xs``."""
+        if self._graph is not None:
+            raise RuntimeError("the chain is captured already")
+        args = (list(xs), dim, pos, cos, sin, list(ys), None if weights is None else list(weights), eps, interleaved)
+        self._calls.append((None, args[0], None, lambda: rotate_heads(*args), None))
+        return self
+
     def _issue(self):
         for mats, xs, ts, ys, mask in self._calls:
-            if len(mats) == 1:
+            if mats is None:
+                ys()
+            elif len(mats) == 1:
                 mats[0].spmspv_into(xs[0], ts[0], ys[0], mask=mask)
             else:
                 spmspv_many(mats, xs, ts, ys, mask=mask)
@@ -483,7 +770,7 @@ class Chain:
         if not self._calls:
             raise RuntimeError("nothing to capture")
         for mats, xs, _, _, _ in self._calls:
-            for m, x in zip(mats, xs):
+            for m, x in zip(mats or [], xs):
                 m.reserve(int(x.shape[0]))
         dev = self._calls[0][1][0].device
         self._issue()  # eager once: every workspace and phase in place

@@ -49,6 +49,12 @@ def build(verbose: bool = False) -> str:
                                    "-o", os.path.join(objdir, "wide.o")]),
         ([cc] + common + device + ["-c", os.path.join(CSRC, "spmm.hip"),
                                    "-o", os.path.join(objdir, "spmm.o")]),
+        ([cc] + common + device + ["-c", os.path.join(CSRC, "spmm_grad.hip"),
+                                   "-o", os.path.join(objdir, "spmm_grad.o")]),
+        ([cc] + common + device + ["-c", os.path.join(CSRC, "adapt.hip"),
+                                   "-o", os.path.join(objdir, "adapt.o")]),
+        ([cc] + common + device + ["-c", os.path.join(CSRC, "heads.hip"),
+                                   "-o", os.path.join(objdir, "heads.o")]),
     ]
     # the sources compile concurrently (the decode kernels' instantiations
     # take most of the time)
@@ -70,7 +76,8 @@ def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
     link = [cc, "-shared", f"--offload-arch={ARCH}", "-o", tmp,
             os.path.join(objdir, "host.o"), os.path.join(objdir, "spdp.o"), os.path.join(objdir, "wide.o"),
-            os.path.join(objdir, "spmm.o"), "-lpthread"]
+            os.path.join(objdir, "spmm.o"), os.path.join(objdir, "spmm_grad.o"), os.path.join(objdir, "adapt.o"),
+            os.path.join(objdir, "heads.o"), "-lpthread"]
     res = subprocess.run(link, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(link)}\n{res.stdout}{res.stderr}")

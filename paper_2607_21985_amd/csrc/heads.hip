@@ -1,0 +1,515 @@
+// Norm and position rotation of the heads of queries and keys, one pass.
+//
+// A head v of `dim` numbers becomes n = v rsqrt(mean v^2 + eps) w (where there
+// are weights w), and each pair (p, q) of its leading 2 half numbers becomes
+// (p c - q s, p s + q c) with the angles of the token's position. Backward: g =
+// the rotation by the negative angle of dy; dw = sum over heads and tokens of
+// g v r with r = rsqrt(...); dv = r (w g - v r^2 mean(w g v)).
+//
+// Bound by memory: each number is read and written once. A group of lanes
+// owns a head and each lane the two vectors of V numbers that rotate into one
+// another (half-split pairs) or any two (neighbours as pairs, and the rest of
+// the head), so the rotation needs no exchange between lanes. A wave keeps its
+// token's angles in registers for several heads.
+
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "internal.h"
+
+namespace {
+
+constexpr int kMaxInputs = 8;
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kMaxDim = 512;
+
+struct HeadsInput {
+  const uint16_t* x;
+  const uint16_t* w;   // NULL: no norm
+  const uint16_t* dy;  // backward
+  uint16_t* y;         // or dx
+  float* part;         // backward with weights: [workgroup of this input][dim]
+  int heads;
+  int wg0;             // the input's first workgroup
+};
+struct HeadsArgs {
+  HeadsInput m[kMaxInputs];
+  const int* pos;
+  const float* cosine;
+  const float* sine;
+  float eps;
+  int inputs;
+  int n_tokens;
+  int positions;
+  int dim, half;
+  int interleaved;
+  int lanes;  // of a head: a power of two
+  int per;    // heads of a group of lanes, one after another
+};
+
+template <int V>
+__device__ __forceinline__ void load_v(const uint16_t* p, float (&v)[V]) {
+  uint16_t h[V];
+  __builtin_memcpy(h, p, 2 * V);
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = __half2float(__ushort_as_half(h[e]));
+}
+template <int V>
+__device__ __forceinline__ void store_v(uint16_t* p, const float (&v)[V]) {
+  uint16_t h[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) h[e] = __half_as_ushort(__float2half_rn(v[e]));
+  __builtin_memcpy(p, h, 2 * V);
+}
+
+// A lane's place in a head: the vectors at a and b (b past the end: none), and
+// how they rotate.
+struct Slot {
+  int a, b;
+  int kind;  // 0: not at all, 1: a with b, 2: neighbours within a and within b
+};
+template <int V>
+__device__ __forceinline__ Slot slot_of(int s, int dim, int half, int interleaved) {
+  Slot t;
+  if (!interleaved && s < half / V) {
+    t.a = s * V;
+    t.b = half + s * V;
+    t.kind = 1;
+  } else {
+    const int from = interleaved ? 0 : half / V;
+    t.a = (interleaved ? 0 : 2 * half) + 2 * V * (s - from);
+    t.b = t.a + V;
+    t.kind = interleaved ? 2 : 0;
+  }
+  return t;
+}
+
+// The rotation of a slot's vectors by the angle's cosine and (sign times) sine.
+template <int V>
+struct Turn {
+  float c[2][V], s[2][V];
+};
+template <int V>
+__device__ __forceinline__ void load_turn(const HeadsArgs& a, const Slot& t, long long pos, float sign, Turn<V>& u) {
+  const float* const c = a.cosine + pos * a.half;
+  const float* const s = a.sine + pos * a.half;
+  if (t.kind == 1) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      u.c[0][e] = c[t.a + e];
+      u.s[0][e] = sign * s[t.a + e];
+    }
+  } else if (t.kind == 2) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int at = k == 0 ? t.a : t.b;
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        const bool in = at + e < 2 * a.half;
+        u.c[k][e] = in ? c[(at + e) / 2] : 1.0f;
+        u.s[k][e] = in ? sign * s[(at + e) / 2] : 0.0f;
+      }
+    }
+  }
+}
+template <int V>
+__device__ __forceinline__ void turn(const Slot& t, const Turn<V>& u, int lead, float (&x)[2][V]) {
+  if (t.kind == 1) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float p = x[0][e], q = x[1][e];
+      x[0][e] = p * u.c[0][e] - q * u.s[0][e];
+      x[1][e] = q * u.c[0][e] + p * u.s[0][e];
+    }
+  } else if (t.kind == 2) {
+    if constexpr (V > 1) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < V; e += 2)
+          if ((k == 0 ? t.a : t.b) + e < lead) {
+            const float p = x[k][e], q = x[k][e + 1];
+            x[k][e] = p * u.c[k][e] - q * u.s[k][e];
+            x[k][e + 1] = q * u.c[k][e] + p * u.s[k][e];
+          }
+    }
+  }
+}
+
+// A workgroup of an input: its groups of lanes take `per` heads of a token
+// each, the groups of a wave all of one token.
+template <int V, int R, bool BACK>
+__global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
+  int which = 0;
+  while (which + 1 < a.inputs && (int)blockIdx.x >= a.m[which + 1].wg0) ++which;
+  const HeadsInput m = a.m[which];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = 64 / a.lanes;
+  const int group = lane / a.lanes, sub = lane % a.lanes;
+  const int chunk = groups * a.per;  // heads of a wave's round
+  const int chunks = (m.heads + chunk - 1) / chunk;
+  const bool norm = m.w != nullptr;
+  const float inv_dim = 1.0f / (float)a.dim;
+
+  Slot t[R];
+  float w[R][2][V];
+  float dw[R][2][V];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    t[r] = slot_of<V>(sub + 64 * r, a.dim, a.half, a.interleaved);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int at = (k == 0 ? t[r].a : t[r].b) + e;
+        w[r][k][e] = norm && at < a.dim ? __half2float(__ushort_as_half(m.w[at])) : 1.0f;
+        dw[r][k][e] = 0.0f;
+      }
+  }
+  const int wgs = (which + 1 < a.inputs ? a.m[which + 1].wg0 : (int)gridDim.x) - m.wg0;
+  const long long rounds = (long long)a.n_tokens * chunks;
+  for (long long q = ((long long)blockIdx.x - m.wg0) * kWaves + wave; q < rounds; q += (long long)wgs * kWaves) {
+    const int tok = (int)(q / chunks);
+    const int h0 = (int)(q % chunks) * chunk;
+    const int pos = a.pos[tok];
+    const bool inside = (unsigned)pos < (unsigned)a.positions;
+    if (!BACK && !inside) continue;  // a padding token
+    Turn<V> u[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) load_turn<V>(a, t[r], inside ? pos : 0, BACK ? -1.0f : 1.0f, u[r]);
+    for (int i = 0; i < a.per; ++i) {
+      const int h = h0 + i * groups + group;
+      const bool on = h < m.heads;
+      const size_t at = ((size_t)tok * m.heads + (on ? h : 0)) * a.dim;
+      float x[R][2][V], g[R][2][V];
+      float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) x[r][k][e] = g[r][k][e] = 0.0f;
+          const int from = k == 0 ? t[r].a : t[r].b;
+          if (on && inside && from < a.dim) {
+            if (!BACK || norm) load_v<V>(m.x + at + from, x[r][k]);
+            if (BACK) load_v<V>(m.dy + at + from, g[r][k]);
+          }
+        }
+        if (BACK) turn<V>(t[r], u[r], 2 * a.half, g[r]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            sum += x[r][k][e] * x[r][k][e];
+            if (BACK) dot += w[r][k][e] * g[r][k][e] * x[r][k][e];
+          }
+      }
+      if (norm) {
+        for (int d = 1; d < a.lanes; d <<= 1) {
+          sum += __shfl_xor(sum, d);
+          if (BACK) dot += __shfl_xor(dot, d);
+        }
+      }
+      // (heads that are none, and padding, would divide by 0 where eps is 0)
+      const float rms = norm && on && inside ? 1.0f / __fsqrt_rn(sum * inv_dim + a.eps) : 1.0f;
+      const float back = rms * rms * (dot * inv_dim);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float o[2][V];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float v = x[r][k][e];
+            if (!BACK) {
+              o[k][e] = norm ? v * rms * w[r][k][e] : v;
+            } else if (norm) {
+              dw[r][k][e] += g[r][k][e] * v * rms;
+              o[k][e] = rms * (w[r][k][e] * g[r][k][e] - v * back);
+            } else {
+              o[k][e] = g[r][k][e];
+            }
+          }
+        if (!BACK) turn<V>(t[r], u[r], 2 * a.half, o);
+        if (on) {
+          if (t[r].a < a.dim) store_v<V>(m.y + at + t[r].a, o[0]);
+          if (t[r].b < a.dim) store_v<V>(m.y + at + t[r].b, o[1]);
+        }
+      }
+    }
+  }
+  if constexpr (BACK) {
+    if (!norm) return;
+    // the groups of a wave, then the waves in order
+    __shared__ float red[kWaves][kMaxDim];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float v = dw[r][k][e];
+          for (int d = a.lanes; d < 64; d <<= 1) v += __shfl_xor(v, d);
+          const int at = (k == 0 ? t[r].a : t[r].b) + e;
+          if (group == 0 && at < a.dim) red[wave][at] = v;
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.dim; i += kThreads)
+      m.part[((size_t)blockIdx.x - m.wg0) * a.dim + i] = ((red[0][i] + red[1][i]) + red[2][i]) + red[3][i];
+  }
+}
+
+// The workgroups' sums, added in a fixed order: each wave every 16th, the
+// waves one after another.
+struct SumArgs {
+  const float* part[kMaxInputs];
+  float* out[kMaxInputs];
+  int n[kMaxInputs];
+  int dim;
+};
+__global__ __launch_bounds__(1024) void heads_sum_kernel(SumArgs a) {
+  __shared__ float red[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i = (int)blockIdx.x * 64 + lane;
+  const int y = blockIdx.y;
+  float sum = 0.0f;
+  if (i < a.dim)
+    for (int q = wave; q < a.n[y]; q += 16) sum += a.part[y][(size_t)q * a.dim + i];
+  red[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && i < a.dim) {
+    for (int w = 1; w < 16; ++w) sum += red[w][lane];
+    a.out[y][i] = sum;
+  }
+}
+
+using spdp::fail;
+
+int hip_fail(hipError_t e, const char* what) {
+  return fail(SPDP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// The numbers that a lane reads at once, and the lanes and workgroups that
+// follow: 16 bytes where the pairs and heads divide into such vectors, else
+// pairs of neighbours, else single numbers (half-split pairs of an odd half).
+// Workgroups: each wave has a token's heads, or so many of them that about
+// four workgroups per CU result.
+struct HeadsPlan {
+  int v, slots, lanes, rounds;  // rounds: slots of a lane
+  int per;
+  int wg0[kMaxInputs + 1];
+};
+void plan_heads(const spdp_heads_t* in, int inputs, const spdp_rotation_t* r, long long n_tokens, bool back, int cus, HeadsPlan* p) {
+  const int half = r->rot / 2;
+  if (r->interleaved ? r->dim % 16 == 0 : half % 8 == 0 && r->dim % 8 == 0)
+    p->v = 8;
+  else
+    p->v = r->interleaved || half % 2 == 0 ? 2 : 1;
+  const int lead = r->interleaved ? 0 : half / p->v;
+  const int rest = r->dim - (r->interleaved ? 0 : r->rot);
+  p->slots = lead + (rest + 2 * p->v - 1) / (2 * p->v);
+  p->lanes = 1;
+  while (p->lanes < p->slots && p->lanes < 64) p->lanes *= 2;
+  p->rounds = (p->slots + 63) / 64;
+  const int groups = 64 / p->lanes;
+  long long all = 0, waves = 4ll * cus * kWaves;
+  for (int i = 0; i < inputs; ++i) all += n_tokens * in[i].heads;
+  p->per = (int)std::max<long long>(1, std::min<long long>(8, all / (groups * waves)));
+  long long rounds[kMaxInputs], sum = 0;
+  for (int i = 0; i < inputs; ++i) {
+    const int chunk = groups * p->per;
+    rounds[i] = n_tokens * ((in[i].heads + chunk - 1) / chunk);
+    sum += rounds[i];
+  }
+  // backward: each workgroup's share of the weights' gradient is written and
+  // read again, so no more of them than fill the card
+  const long long most = back ? 8ll * cus : 1ll << 30;
+  p->wg0[0] = 0;
+  for (int i = 0; i < inputs; ++i) {
+    const long long want = (rounds[i] + kWaves - 1) / kWaves;
+    p->wg0[i + 1] = p->wg0[i] + (int)std::max<long long>(1, std::min(want, most * rounds[i] / std::max<long long>(1, sum)));
+  }
+}
+
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+int check(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int64_t n_tokens) {
+  if (!in || !r) return fail(SPDP_ERR_INVALID_ARG, "inputs or rotation is NULL");
+  if (inputs < 1 || inputs > kMaxInputs) return fail(SPDP_ERR_INVALID_ARG, "the number of inputs must lie in [1, 8]");
+  if (!r->positions || !r->cosine || !r->sine) return fail(SPDP_ERR_INVALID_ARG, "positions, cosine or sine is NULL");
+  if (n_tokens < 1 || r->table < 1) return fail(SPDP_ERR_INVALID_ARG, "n_tokens and table must be at least 1");
+  if (n_tokens > 1 << 24 || r->table > 1 << 30) return fail(SPDP_ERR_UNSUPPORTED, "more than 2^24 tokens or 2^30 positions");
+  if (r->dim < 2 || r->rot < 2 || r->dim % 2 || r->rot % 2 || r->rot > r->dim)
+    return fail(SPDP_ERR_INVALID_ARG, "dim and rot must be even, with 2 <= rot <= dim");
+  if (r->dim > kMaxDim) return fail(SPDP_ERR_UNSUPPORTED, "heads of more than 512 numbers");
+  if (!(r->eps >= 0.0f) || r->eps > 1e30f) return fail(SPDP_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+  for (int i = 0; i < inputs; ++i) {
+    if (!in[i].x) return fail(SPDP_ERR_INVALID_ARG, "x is NULL");
+    if (in[i].heads < 1) return fail(SPDP_ERR_INVALID_ARG, "heads must be at least 1");
+    if (in[i].heads > 65536) return fail(SPDP_ERR_UNSUPPORTED, "more than 65536 heads");
+  }
+  return SPDP_OK;
+}
+
+template <int V, int R>
+void launch(const HeadsArgs& a, bool back, dim3 grid, hipStream_t s) {
+  if (back)
+    hipLaunchKernelGGL((heads_kernel<V, R, true>), grid, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((heads_kernel<V, R, false>), grid, dim3(kThreads), 0, s, a);
+}
+
+int compute_units(int* cus) {
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+  e = hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) return hip_fail(e, "hipDeviceGetAttribute");
+  *cus = std::max(1, *cus);
+  return SPDP_OK;
+}
+
+bool overlap(const void* p, size_t np, const void* q, size_t nq) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && a < b + nq && b < a + np;
+}
+
+size_t grad_bytes(const spdp_heads_t* in, int inputs, int dim, const HeadsPlan& p) {
+  size_t bytes = 0;
+  for (int i = 0; i < inputs; ++i)
+    if (in[i].weight) bytes += aligned((size_t)(p.wg0[i + 1] - p.wg0[i]) * dim * 4);
+  return bytes;
+}
+
+int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int64_t n_tokens, bool back, void* workspace,
+          size_t workspace_bytes, void* stream) {
+  int st = check(in, inputs, r, n_tokens);
+  if (st != SPDP_OK) return st;
+  // an output may be its own input as a whole, and overlaps nothing else
+  for (int i = 0; i < inputs; ++i) {
+    if (!in[i].y) return fail(SPDP_ERR_INVALID_ARG, "y is NULL");
+    if (back && !in[i].dy) return fail(SPDP_ERR_INVALID_ARG, "dy is NULL");
+    if (back && (in[i].weight != nullptr) != (in[i].dweight != nullptr))
+      return fail(SPDP_ERR_INVALID_ARG, "dweight goes with weight");
+    const size_t row = (size_t)n_tokens * r->dim * 2, n = row * in[i].heads;
+    for (int j = 0; j < inputs; ++j) {
+      const size_t other = row * in[j].heads;
+      if (overlap(in[i].y, n, in[j].x, other) && !(i == j && in[i].y == in[j].x))
+        return fail(SPDP_ERR_INVALID_ARG, "an output overlaps an input");
+      if (back && overlap(in[i].y, n, in[j].dy, other) && !(i == j && in[i].y == in[j].dy))
+        return fail(SPDP_ERR_INVALID_ARG, "an output overlaps an input");
+      if (i != j && overlap(in[i].y, n, in[j].y, other)) return fail(SPDP_ERR_INVALID_ARG, "outputs overlap");
+      if (overlap(in[i].y, n, in[j].weight, (size_t)r->dim * 2)) return fail(SPDP_ERR_INVALID_ARG, "an output overlaps a weight");
+    }
+    if (overlap(in[i].y, n, r->positions, (size_t)n_tokens * 4) ||
+        overlap(in[i].y, n, r->cosine, (size_t)r->table * r->rot * 2) || overlap(in[i].y, n, r->sine, (size_t)r->table * r->rot * 2))
+      return fail(SPDP_ERR_INVALID_ARG, "an output overlaps the positions or the tables");
+  }
+  int cus = 1;
+  st = compute_units(&cus);
+  if (st != SPDP_OK) return st;
+  HeadsPlan p;
+  plan_heads(in, inputs, r, n_tokens, back, cus, &p);
+  HeadsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  SumArgs sum;
+  std::memset(&sum, 0, sizeof(sum));
+  sum.dim = r->dim;
+  int sums = 0;
+  if (back) {
+    const size_t need = grad_bytes(in, inputs, r->dim, p);
+    if (need > 0) {
+      if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
+      if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(SPDP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+      if (workspace_bytes < need)
+        return fail(SPDP_ERR_INVALID_ARG,
+                    "workspace of " + std::to_string(workspace_bytes) + " bytes, " + std::to_string(need) + " needed");
+    }
+  }
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  for (int i = 0; i < inputs; ++i) {
+    a.m[i] = HeadsInput{in[i].x, in[i].weight, in[i].dy, in[i].y, nullptr, in[i].heads, p.wg0[i]};
+    if (back && in[i].weight) {
+      const int wgs = p.wg0[i + 1] - p.wg0[i];
+      a.m[i].part = reinterpret_cast<float*>(ws);
+      sum.part[sums] = a.m[i].part;
+      sum.out[sums] = in[i].dweight;
+      sum.n[sums++] = wgs;
+      ws += aligned((size_t)wgs * r->dim * 4);
+    }
+  }
+  a.pos = r->positions;
+  a.cosine = r->cosine;
+  a.sine = r->sine;
+  a.eps = r->eps;
+  a.inputs = inputs;
+  a.n_tokens = (int)n_tokens;
+  a.positions = (int)r->table;
+  a.dim = r->dim;
+  a.half = r->rot / 2;
+  a.interleaved = r->interleaved != 0;
+  a.lanes = p.lanes;
+  a.per = p.per;
+  const dim3 grid((unsigned)p.wg0[inputs]);
+  auto s = static_cast<hipStream_t>(stream);
+  if (p.v == 8)
+    launch<8, 1>(a, back, grid, s);
+  else if (p.v == 2 && p.rounds == 1)
+    launch<2, 1>(a, back, grid, s);
+  else if (p.v == 2)
+    launch<2, 2>(a, back, grid, s);
+  else
+    launch<1, 4>(a, back, grid, s);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && sums > 0) {
+    hipLaunchKernelGGL(heads_sum_kernel, dim3((unsigned)((r->dim + 63) / 64), (unsigned)sums), dim3(1024), 0, s, sum);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");
+}
+
+template <class F>
+int guarded(F f) {
+  try {
+    spdp::clear_error();
+    return f();
+  } catch (...) {  // a message found no memory
+    return SPDP_ERR_OOM;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int spdp_rotate_heads(const spdp_heads_t* inputs, int32_t n_inputs, const spdp_rotation_t* rotation, int64_t n_tokens,
+                      void* stream) {
+  return guarded([&] { return heads(inputs, n_inputs, rotation, n_tokens, false, nullptr, 0, stream); });
+}
+
+int spdp_rotate_heads_grad_workspace(const spdp_heads_t* inputs, int32_t n_inputs, const spdp_rotation_t* rotation,
+                                     int64_t n_tokens, size_t* bytes) {
+  return guarded([&] {
+    if (!bytes) return fail(SPDP_ERR_INVALID_ARG, "bytes is NULL");
+    int st = check(inputs, n_inputs, rotation, n_tokens);
+    int cus = 1;
+    if (st == SPDP_OK) st = compute_units(&cus);
+    if (st != SPDP_OK) return st;
+    HeadsPlan p;
+    plan_heads(inputs, n_inputs, rotation, n_tokens, true, cus, &p);
+    *bytes = grad_bytes(inputs, n_inputs, rotation->dim, p);
+    return (int)SPDP_OK;
+  });
+}
+
+int spdp_rotate_heads_grad(const spdp_heads_t* inputs, int32_t n_inputs, const spdp_rotation_t* rotation,
+                           int64_t n_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+  return guarded([&] { return heads(inputs, n_inputs, rotation, n_tokens, true, workspace, workspace_bytes, stream); });
+}
+
+}  // extern "C"
