@@ -279,7 +279,7 @@ int spdp_spmm(spdp_handle_t h, const uint16_t* X, int64_t n_tokens,
  * a workspace of its own. Where the grid leaves compute units idle the stripes
  * are split into ranges, whose fp32 sums a second kernel adds in order: the
  * summation order depends on the matrix, the token count and the device's
- * compute-unit count alone (and on the tuning variables SPDP_GRAD_TOKENS and
+ * compute-unit count alone (and on the tuning variables SPDP_GRAD_FORM and
  * SPDP_GRAD_SPLITS, when set).
  */
 int spdp_spmm_grad_workspace(spdp_handle_t h, int64_t n_tokens, size_t* bytes);

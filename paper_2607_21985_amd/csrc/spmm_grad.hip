@@ -111,34 +111,55 @@ __global__ __launch_bounds__(kThreads) void grad_plain_kernel(GradArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// The form for handles with word records. Four waves own 128 columns (two
-// chunks) and 32 TB tokens; wave w has the columns 32 w .. + 31, lane l column
-// l mod 32 and, of each 64-row word, the rows 32 (l / 32) .. + 31. Per four
-// rows a lane reads the next four values of its column from LDS (at any 2-byte
-// address: as many are used as the four bits of the bitmap word have ones) and
-// puts them into their places with two byte permutations, whose selectors a
-// table of 16 entries holds. Eight rows are an operand of
-// v_mfma_f32_32x32x16_f16; the tokens' operands come from LDS in the same order
-// of rows.
+// The form for handles with word records. CG TG waves own 32 CG columns (CG / 2
+// chunks) and 32 TB TG tokens, each wave 32 columns and 32 TB tokens; lane l has
+// column l mod 32 and, of each 64-row word, the rows 32 (l / 32) .. + 31. Per
+// four rows a lane reads the next four values of its column from LDS (as many
+// are used as the four bits of the bitmap word have ones) and puts them into
+// their places with two byte permutations, whose selectors a table of 16 entries
+// holds. Eight rows are an operand of v_mfma_f32_32x32x16_f16; the tokens'
+// operands come from LDS in the same order of rows. The values are read as two
+// aligned 8-byte words and shifted in registers: a wave's 64 reads of 8 bytes
+// take 6 cycles where all are aligned, 65 where they are not.
 //
-// Per stripe the two chunks' values (one contiguous run) arrive by DMA one
-// stripe ahead, a quarter with each word; per word the tokens' 64 rows of dY,
-// one word ahead, 16-byte piece p of token t at place p ^ (t mod 8).
+// A step is 8 rows of both halves of the lanes; a word has four. During the
+// MFMAs of a step the next one's operands are built and read, across words, too.
+// Values (per stripe one contiguous run) arrive by DMA in three parts during the
+// stripe before, the tokens' 64 rows of dY one word ahead, 16-byte piece p of
+// token t at place p ^ (t / 2 mod 8). The one barrier per word stands before
+// its last step, when all of the word's operands have been read: what is
+// requested behind it may overwrite them.
 
-template <int TB>
+template <int TB, int CG, int TG>
 struct GradCfg {
-  static constexpr int kTokens = 32 * TB;
+  static constexpr int kWaves = CG * TG;
+  static constexpr int kTokens = 32 * TB * TG;
   static constexpr int kDyBytes = kTokens * 128;
-  static int lds(int slot) { return 4 * slot + 2 * kDyBytes + 256; }
+  static int lds(int slot) { return CG * slot + 2 * kDyBytes + 256; }
 };
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ u32x2 lds_read8(uint32_t at) {
-  u32x2 v;
-  __builtin_memcpy(&v, (const __attribute__((address_space(3))) unsigned char*)(uintptr_t)at, 8);
-  return v;
-}
+// Four rows of a column: the 16 bytes of LDS that hold its next four values,
+// and the selectors for the rows' bits.
+struct Quad {
+  u32x2 a, b, sel;
+  uint32_t p;
+  __device__ __forceinline__ void read(uint32_t at, uint32_t selectors_at) {
+    typedef const __attribute__((address_space(3))) u32x2* lds8;
+    p = at;
+    a = *(lds8)(uintptr_t)(at & ~7u);
+    b = *(lds8)(uintptr_t)((at & ~7u) + 8u);
+    sel = *(lds8)(uintptr_t)selectors_at;
+  }
+  // the rows' fp16, 0 where the bit is clear
+  __device__ __forceinline__ u32x2 rows() const {
+    const bool up = p & 4u;
+    const uint32_t x0 = up ? a[1] : a[0], x1 = up ? b[0] : a[1], x2 = up ? b[1] : b[0];
+    const uint32_t lo = __builtin_amdgcn_alignbyte(x1, x0, p), hi = __builtin_amdgcn_alignbyte(x2, x1, p);
+    return u32x2{__builtin_amdgcn_perm(hi, lo, sel[0]), __builtin_amdgcn_perm(hi, lo, sel[1])};
+  }
+};
 
 // selectors of the two dwords of four rows with bitmap bits `b`
 __device__ __forceinline__ u32x2 selectors(uint32_t b) {
@@ -153,22 +174,30 @@ __device__ __forceinline__ u32x2 selectors(uint32_t b) {
   return s;
 }
 
+// Where a lane is in its column: the bits of the word's rows that it has, and
+// the LDS address of the next value.
+struct Walk {
+  uint32_t mask, p;
+};
+
 // DYV: dY rows are 16-byte aligned (else they are read at any address)
-template <int TB, bool DYV>
-__global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
-  using C = GradCfg<TB>;
+template <int TB, int CG, int TG, bool DYV>
+__global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
+  using C = GradCfg<TB, CG, TG>;
+  constexpr int W = C::kWaves;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cg = wave % CG, tg = wave / CG;
   const int half = lane >> 5;
   const long long nb0 = (long long)blockIdx.y * C::kTokens;
   const int last_tok = (int)min(a.n_tokens - nb0, (long long)C::kTokens) - 1;
-  const int chunk0 = 2 * (int)blockIdx.x;
-  const int chunk1 = min(chunk0 + 2, a.chunks);
-  const int chunk = chunk0 + (wave >> 1);
-  const bool on = chunk < chunk1;  // the last workgroup's second chunk may be none
+  const int chunk0 = CG / 2 * (int)blockIdx.x;
+  const int chunk1 = min(chunk0 + CG / 2, a.chunks);
+  const bool on = chunk0 + (cg >> 1) < chunk1;  // the last workgroup's chunks may be fewer
+  const int chunk = on ? chunk0 + (cg >> 1) : chunk0;
   const uint32_t l0 = lds_addr(lds);
-  const uint32_t val = l0, dyl = l0 + 4u * (uint32_t)a.slot, lut = dyl + 2 * C::kDyBytes;
+  const uint32_t val = l0, dyl = l0 + (uint32_t)(CG * a.slot), lut = dyl + 2 * C::kDyBytes;
   if (threadIdx.x < 16) {
     const u32x2 s = selectors(threadIdx.x);
     *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(lut + 8 * threadIdx.x) = s;
@@ -176,25 +205,41 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
   const int r0 = (int)blockIdx.z * a.per, r1 = min(a.n_stripes, r0 + a.per);
   const uint16_t* const dyb = a.dy + nb0 * (long long)a.rows;
 
-  // the part `q` of 4 of stripe r's values, [t0, t1) of the values' bytes
-  auto issue_values = [&](int r, int q, uint32_t t0, uint32_t t1) __attribute__((always_inline)) {
-    if (t1 <= t0) return;
-    const uint32_t last = t1 - t0 - 16u;
-    const uint32_t to = val + (uint32_t)(r & 1) * 2u * (uint32_t)a.slot;
-    for (uint32_t at = 1024u * (uint32_t)(4 * q + wave); at <= last; at += 16384u)
-      dma16(a.values, t0 + min(at + 16u * (uint32_t)lane, last),
+  // The byte offsets of a stripe's values: the workgroup's first chunk, the
+  // wave's, and the end.
+  struct Run {
+    uint32_t t0, tm, t1;
+  };
+  const const_ptr<uint32_t> co = (const_ptr<uint32_t>)a.chunk_off;
+  auto run_of = [&](int r) __attribute__((always_inline)) {
+    const size_t at = (size_t)min(r, r1 - 1) * a.chunks;
+    return Run{co[at + chunk0], co[at + chunk], co[at + chunk1]};
+  };
+  // the part q of 3 of stripe r's values
+  auto issue_values = [&](int r, int q, const Run& u) __attribute__((always_inline)) {
+    if (r >= r1 || u.t1 <= u.t0) return;
+    const uint32_t last = u.t1 - u.t0 - 16u;
+    const uint32_t to = val + (uint32_t)(r & 1) * (uint32_t)(CG / 2) * (uint32_t)a.slot;
+    for (uint32_t at = 1024u * (uint32_t)(W * q + wave); at <= last; at += 3072u * W)
+      dma16(a.values, u.t0 + min(at + 16u * (uint32_t)lane, last),
             (uint32_t)__builtin_amdgcn_readfirstlane((int)(to + at)));
   };
-  const int piece = (lane & 7) ^ (lane >> 3);
-  // 64 rows of dY from row m0 on into buffer b
-  auto issue_dy = [&](int m0, int b) __attribute__((always_inline)) {
+  const int piece = (lane & 7) ^ (4 * (wave & 1) + (lane >> 4));
+  // the 64 rows of word `word` (from the matrix's first) of dY into buffer b: 8
+  // tokens a wave and round
+  auto issue_dy = [&](int word, int b) __attribute__((always_inline)) {
+    if (word >= 4 * r1) return;
 #pragma unroll
-    for (int i = 0; i < TB; ++i) {
-      const uint32_t to = dyl + (uint32_t)(b * C::kDyBytes + (32 * i + 8 * wave) * 128);
-      const uint32_t t = (uint32_t)min(32 * i + 8 * wave + (lane >> 3), last_tok);
-      const int m = m0 + 8 * piece;
+    for (int i = 0; i < (4 * TB * TG + W - 1) / W; ++i) {
+      const int t8 = W * i + wave;
+      if (4 * TB * TG % W != 0 && t8 >= 4 * TB * TG) break;
+      const uint32_t to = dyl + (uint32_t)(b * C::kDyBytes + t8 * 1024);
+      int lane8 = lane >> 3;
+      asm volatile("" : "+v"(lane8));  // (keeps the tokens' offsets out of registers between words)
+      const uint32_t t = (uint32_t)min(8 * t8 + lane8, last_tok);
+      const int m = 64 * word + 8 * piece;
       if constexpr (DYV) {
-        if (m < a.rows)
+        if (64 * word + 64 <= a.rows || m < a.rows)
           dma16(dyb, (t * (uint32_t)a.rows + (uint32_t)m) * 2u, (uint32_t)__builtin_amdgcn_readfirstlane((int)to));
         else
           *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + 16u * (uint32_t)lane) = u32x4{0, 0, 0, 0};
@@ -205,90 +250,113 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(GradArgs a) {
       }
     }
   };
-  // the lane's record of stripe r, word v: its column's word and the byte
-  // offset of the word's first value in the chunk
+  // the lane's record of a word: its column's bits and, for a pair of columns,
+  // the byte offsets of the word's first value in the chunk
   struct Rec {
-    uint64_t word;
-    uint32_t off;
+    uint32_t lo, hi, offs;
   };
+  const unsigned char* const rec_at =
+      a.rec + (size_t)chunk * kChunkRecBytes + (4 * (2 * (cg & 1) + (lane >> 4 & 1))) * kRecBytes;
   const int c16 = lane & 15;
-  const int group = 2 * (wave & 1) + (lane >> 4 & 1);
-  auto load_rec1 = [&](int r, int v, Rec& m) __attribute__((always_inline)) {
-    const unsigned char* p =
-        a.rec + ((size_t)r * a.chunks + (on ? chunk : chunk0)) * kChunkRecBytes + (4 * group + v) * kRecBytes;
-    m.word = *reinterpret_cast<const uint64_t*>(p + 8 * c16);
-    m.off = *reinterpret_cast<const uint16_t*>(p + 128 + 2 * c16);
+  auto load_rec1 = [&](int word, Rec& m) __attribute__((always_inline)) {
+    word = min(word, 4 * r1 - 1);
+    const unsigned char* p = rec_at + (size_t)(word >> 2) * a.chunks * kChunkRecBytes + (word & 3) * kRecBytes;
+    const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * c16);
+    m.lo = w.x;
+    m.hi = w.y;
+    m.offs = *reinterpret_cast<const uint32_t*>(p + 128 + 4 * (c16 >> 1));
+  };
+  auto walk = [&](const Rec& m, int r, const Run& u) __attribute__((always_inline)) {
+    Walk k;
+    k.mask = half ? m.hi : m.lo;
+    k.p = val + (uint32_t)(r & 1) * (uint32_t)(CG / 2) * (uint32_t)a.slot + (u.tm - u.t0) +
+          ((lane & 1) ? m.offs >> 16 : m.offs & 0xFFFFu) +
+          (half ? 2u * (uint32_t)__builtin_popcount(m.lo) : 0u);
+    return k;
   };
 
   float16v acc[TB];
 #pragma unroll
   for (int j = 0; j < TB; ++j) acc[j] = float16v{};
-  const const_ptr<uint32_t> co = (const_ptr<uint32_t>)a.chunk_off;
-
-  Rec cur, nxt;
-  uint32_t t0 = co[(size_t)r0 * a.chunks + chunk0], tm = co[(size_t)r0 * a.chunks + (on ? chunk : chunk0)],
-           t1 = co[(size_t)r0 * a.chunks + chunk1];
+  Run here = run_of(r0), next = run_of(r0 + 1);
+  Rec rec, rec1, rec2;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) issue_values(r0, q, t0, t1);
-  issue_dy(r0 * kTM, 0);
-  load_rec1(r0, 0, cur);
-  for (int r = r0; r < r1; ++r) {
-    // the chunk's values in LDS
-    const uint32_t mine = val + (uint32_t)(r & 1) * 2u * (uint32_t)a.slot + (tm - t0);
-    const bool more = r + 1 < r1;
-    uint32_t n0 = 0, nm = 0, n1 = 0;
-    if (more) {
-      const size_t at = (size_t)(r + 1) * a.chunks;
-      n0 = co[at + chunk0];
-      nm = co[at + (on ? chunk : chunk0)];
-      n1 = co[at + chunk1];
+  for (int q = 0; q < 3; ++q) issue_values(r0, q, here);
+  issue_dy(4 * r0, 0);
+  issue_dy(4 * r0 + 1, 1);
+  load_rec1(4 * r0, rec1);
+  load_rec1(4 * r0 + 1, rec2);
+  load_rec1(4 * r0 + 2, rec);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  issue_values(r0 + 1, 0, next);
+  Walk k0 = walk(rec1, r0, here), k1 = walk(rec2, r0, here);
+
+  half8 x[2][TB];
+  Quad q[2];
+  const uint32_t db = dyl + (uint32_t)(4096 * TB * tg) + 128u * (uint32_t)(lane & 31);
+  auto read_x = [&](int v, int j, int t) __attribute__((always_inline)) {
+    const uint32_t place = 16u * (uint32_t)((4 * half + j) ^ (lane >> 1 & 7));
+    return *(const __attribute__((address_space(3))) half8*)(uintptr_t)(db + (uint32_t)((v & 1) * C::kDyBytes) + 4096u * t + place);
+  };
+  auto read_q = [&](Walk& k, int j) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t b = k.mask >> (8 * j + 4 * i) & 15u;
+      q[i].read(k.p, lut + 8u * b);
+      k.p += 2u * (uint32_t)__builtin_popcount(b);
     }
+  };
+  u32x2 w[2];
+  read_q(k0, 0);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) w[i] = q[i].rows();
+  read_q(k0, 1);
+#pragma unroll
+  for (int t = 0; t < TB; ++t) x[0][t] = read_x(0, 0, t);
+
+  for (int r = r0; r < r1; ++r) {
+    Run after;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (v < 3)
-        issue_dy(r * kTM + 64 * (v + 1), (v + 1) & 1);
-      else if (more)
-        issue_dy((r + 1) * kTM, 0);
-      if (more) issue_values(r + 1, v, n0, n1);
-      if (v < 3)
-        load_rec1(r, v + 1, nxt);
-      else if (more)
-        load_rec1(r + 1, 0, nxt);
-      if (on) {
-        const uint32_t lo = (uint32_t)cur.word;
-        const uint32_t mask = half ? (uint32_t)(cur.word >> 32) : lo;
-        uint32_t p = mine + cur.off + (half ? 2u * (uint32_t)__builtin_popcount(lo) : 0u);
-        const uint32_t db = dyl + (uint32_t)((v & 1) * C::kDyBytes) + 128u * (uint32_t)(lane & 31);
+      Walk k2;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t b0 = mask >> (8 * j) & 15u, b1 = mask >> (8 * j + 4) & 15u;
-          const uint32_t p1 = p + 2u * (uint32_t)__builtin_popcount(b0);
-          const u32x2 v0 = lds_read8(p), v1 = lds_read8(p1);
-          p = p1 + 2u * (uint32_t)__builtin_popcount(b1);
-          const u32x2 s0 = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)(lut + 8u * b0);
-          const u32x2 s1 = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)(lut + 8u * b1);
-          const half8 w = __builtin_bit_cast(
-              half8, u32x4{__builtin_amdgcn_perm(v0[1], v0[0], s0[0]), __builtin_amdgcn_perm(v0[1], v0[0], s0[1]),
-                           __builtin_amdgcn_perm(v1[1], v1[0], s1[0]), __builtin_amdgcn_perm(v1[1], v1[0], s1[1])});
-          const uint32_t place = 16u * (uint32_t)((4 * half + j) ^ (lane & 7));
+      for (int j = 0; j < 4; ++j) {
+        if (j == 3) {
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          // the record is there: taken now, for the compiler's own wait for it
+          // would count the loads requested below
+          asm volatile("" : "+v"(rec.lo), "+v"(rec.hi), "+v"(rec.offs));
+          k2 = walk(rec, v < 2 ? r : r + 1, v < 2 ? here : next);
+          load_rec1(4 * r + v + 3, rec);
+          issue_dy(4 * r + v + 2, v & 1);
+          if (v == 3)
+            issue_values(r + 2, 0, after);
+          else if (v < 2)
+            issue_values(r + 1, v + 1, next);
+        }
+        if (v == 2 && j == 0) after = run_of(r + 2);
+        const half8 now = __builtin_bit_cast(half8, u32x4{w[0][0], w[0][1], w[1][0], w[1][1]});
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int t = 0; t < TB; ++t) {
-            const half8 x = *(const __attribute__((address_space(3))) half8*)(uintptr_t)(db + 4096u * t + place);
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w, acc[t], 0, 0, 0);
-          }
+        for (int t = 0; t < TB; ++t) {
+          x[(j + 1) & 1][t] = read_x(j < 3 ? v : v + 1, (j + 1) & 3, t);
+          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[j & 1][t], now, acc[t], 0, 0, 0);
+          if (t == 0) w[0] = q[0].rows();
+          if (t == (TB > 1 ? 1 : 0)) w[1] = q[1].rows();
+          if (t == (TB > 2 ? 2 : TB - 1)) read_q(j < 2 ? k0 : k1, (j + 2) & 3);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
-      cur = nxt;
+      k0 = k1;
+      k1 = k2;
     }
-    t0 = n0;
-    tm = nm;
-    t1 = n1;
+    here = next;
+    next = after;
   }
   if (!on) return;
-  const int col = chunk * kChunkCols + 32 * (wave & 1) + (lane & 31);
+  const int col = chunk * kChunkCols + 32 * (cg & 1) + (lane & 31);
 #pragma unroll
-  for (int t = 0; t < TB; ++t) store_sums(a, acc[t], nb0 + 32 * t, col);
+  for (int t = 0; t < TB; ++t) store_sums(a, acc[t], nb0 + 32 * (TB * tg + t), col);
 }
 
 // ---------------------------------------------------------------------------
@@ -302,68 +370,73 @@ int hip_fail(hipError_t e, const char* what) {
 
 constexpr int kLdsMax = 160 * 1024;
 
+// The forms: blocks of 32 tokens of a wave, groups of 32 columns and groups of
+// tokens of a workgroup.
+struct Form {
+  int tb, cg, tg;
+  int tokens() const { return 32 * tb * tg; }
+  int lds(int slot) const { return cg * slot + 2 * tokens() * 128 + 256; }
+};
+constexpr Form kForms[] = {{1, 4, 1}, {2, 4, 1}, {4, 4, 1}, {4, 4, 2}, {1, 8, 1}, {2, 8, 1}, {4, 8, 1}, {8, 8, 1}};
+constexpr int kNumForms = sizeof(kForms) / sizeof(kForms[0]);
+
 struct GradPlan {
-  int tb;  // 0: plain
+  int form;  // -1: plain
   long long tiles;
   int blocks, per, splits;
 };
 
-int lds_bytes(int tb, int slot) {
-  return tb == 1 ? GradCfg<1>::lds(slot) : tb == 2 ? GradCfg<2>::lds(slot) : tb == 4 ? GradCfg<4>::lds(slot) : GradCfg<8>::lds(slot);
+int env_int(const char* name, int otherwise) {
+  const char* env = std::getenv(name);
+  return env ? std::atoi(env) : otherwise;
 }
 
 void plan_grad(const spdp_matrix* h, long long n_tokens, GradPlan* p) {
   const int cus = std::max(1, h->cus);
-  int forced = 0, forced_tb = -1;
-  if (const char* env = std::getenv("SPDP_GRAD_SPLITS")) forced = std::max(1, std::atoi(env));
-  if (const char* env = std::getenv("SPDP_GRAD_TOKENS")) forced_tb = std::atoi(env) / 32;
+  const int forced_splits = env_int("SPDP_GRAD_SPLITS", 0), forced_form = env_int("SPDP_GRAD_FORM", -2);
   const long long stripes = h->n_stripes;
-  auto fits = [&](int tb) {
-    return h->d_rec != nullptr && lds_bytes(tb, h->chunk_bytes) <= kLdsMax &&
-           std::min<long long>(n_tokens, 32 * tb) * h->rows * 2 <= 1ll << 32 && (n_tokens + 32 * tb - 1) / (32 * tb) <= 65535;
-  };
-  auto fill = [&](int tb) {
-    p->tb = tb;
-    const int tokens = tb ? 32 * tb : 128;
-    p->tiles = (n_tokens + tokens - 1) / tokens;
-    p->blocks = tb ? (h->chunks + 1) / 2 : (int)((h->cols + 63) / 64);
-    const long long wgs = p->tiles * p->blocks;
-    const long long want = forced ? forced : std::max<long long>(1, std::min<long long>(16, cus / wgs));
-    p->per = (int)((stripes + std::min(want, stripes) - 1) / std::min(want, stripes));
-    p->splits = (int)((stripes + p->per - 1) / p->per);
-  };
-  if (forced_tb >= 0) {
-    const int tb = forced_tb >= 8 ? 8 : forced_tb >= 4 ? 4 : forced_tb >= 2 ? 2 : forced_tb;
-    fill(tb > 0 && fits(tb) ? tb : 0);
-    return;
+  p->form = -1;
+  for (int i = 0; i < kNumForms; ++i) {
+    if (forced_form > -2 && forced_form != i) continue;
+    const Form& f = kForms[i];
+    if (h->d_rec == nullptr || f.lds(h->chunk_bytes) > kLdsMax ||
+        std::min<long long>(n_tokens, f.tokens()) * h->rows * 2 > 1ll << 32 || (n_tokens + f.tokens() - 1) / f.tokens() > 65535)
+      continue;
+    if (p->form < 0 || f.tokens() <= n_tokens) p->form = i;
   }
-  int best = 0;
-  for (int tb = 1; tb <= 8; tb *= 2) {
-    if (!fits(tb)) continue;
-    if (best == 0 || 32 * tb <= n_tokens) best = tb;
-  }
-  fill(best);
+  const int tokens = p->form >= 0 ? kForms[p->form].tokens() : 128, columns = p->form >= 0 ? 32 * kForms[p->form].cg : 64;
+  p->tiles = (n_tokens + tokens - 1) / tokens;
+  p->blocks = (int)((h->cols + columns - 1) / columns);
+  const long long wgs = p->tiles * p->blocks;
+  const long long want = std::min<long long>(stripes, forced_splits > 0 ? forced_splits : std::max<long long>(1, std::min<long long>(16, cus / wgs)));
+  p->per = (int)((stripes + want - 1) / want);
+  p->splits = (int)((stripes + p->per - 1) / p->per);
 }
 
 size_t part_bytes(const spdp_matrix* h, long long n_tokens, const GradPlan& p) {
   return p.splits > 1 ? (size_t)p.splits * n_tokens * h->cols * 4 : 0;
 }
 
-template <int TB, bool DYV>
+template <int TB, int CG, int TG, bool DYV>
 hipError_t launch_form(const GradArgs& a, dim3 grid, hipStream_t st) {
-  const int lds = GradCfg<TB>::lds(a.slot);
-  const auto kernel = grad_kernel<TB, DYV>;
+  const int lds = GradCfg<TB, CG, TG>::lds(a.slot);
+  const auto kernel = grad_kernel<TB, CG, TG, DYV>;
   if (lds > 64 * 1024) {
     const hipError_t e =
         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, st, a);
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * CG * TG), lds, st, a);
   return hipGetLastError();
 }
-template <int TB>
-hipError_t launch_tb(const GradArgs& a, dim3 grid, hipStream_t st) {
-  return a.rows % 8 == 0 ? launch_form<TB, true>(a, grid, st) : launch_form<TB, false>(a, grid, st);
+template <int I>
+hipError_t launch_forms(int form, const GradArgs& a, dim3 grid, hipStream_t st) {
+  if constexpr (I < kNumForms) {
+    constexpr Form f = kForms[I];
+    if (form != I) return launch_forms<I + 1>(form, a, grid, st);
+    return a.rows % 8 == 0 ? launch_form<f.tb, f.cg, f.tg, true>(a, grid, st) : launch_form<f.tb, f.cg, f.tg, false>(a, grid, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 int check(const spdp_matrix* h, int64_t n_tokens) {
@@ -423,14 +496,11 @@ int spmm_grad(spdp_handle_t h, const uint16_t* dY, int64_t n_tokens, uint16_t* d
   a.slot = h->chunk_bytes;
   auto s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)p.blocks, (unsigned)p.tiles, (unsigned)p.splits);
-  switch (p.tb) {
-    case 1: e = launch_tb<1>(a, grid, s); break;
-    case 2: e = launch_tb<2>(a, grid, s); break;
-    case 4: e = launch_tb<4>(a, grid, s); break;
-    case 8: e = launch_tb<8>(a, grid, s); break;
-    default:
-      hipLaunchKernelGGL(grad_plain_kernel, grid, dim3(kThreads), 0, s, a);
-      e = hipGetLastError();
+  if (p.form >= 0) {
+    e = launch_forms<0>(p.form, a, grid, s);
+  } else {
+    hipLaunchKernelGGL(grad_plain_kernel, grid, dim3(kThreads), 0, s, a);
+    e = hipGetLastError();
   }
   if (e == hipSuccess && p.splits > 1)
     e = spdp::launch_reduce(a.part, p.splits, n_tokens * h->cols, dX, s);

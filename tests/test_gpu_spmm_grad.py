@@ -70,13 +70,13 @@ def test_exact(rows, cols, tile_k, sw, n):
     m.close()
 
 
-@pytest.mark.parametrize("tokens", [0, 32, 64, 128, 256])
+@pytest.mark.parametrize("form", range(-1, 8))
 @pytest.mark.parametrize("splits", [1, 3, 100])
-def test_every_form_and_split(monkeypatch, tokens, splits):
-    monkeypatch.setenv("SPDP_GRAD_TOKENS", str(tokens))
+def test_every_form_and_split(monkeypatch, form, splits):
+    monkeypatch.setenv("SPDP_GRAD_FORM", str(form))
     monkeypatch.setenv("SPDP_GRAD_SPLITS", str(splits))
     for rows, cols, sw, n in ((1000, 200, 0.5, 300), (803, 333, 0.6, 70), (520, 136, 0.3, 31)):
-        print(f"[gpu] spmm_grad {rows}x{cols} {n} form {tokens} splits {splits}", flush=True)
+        print(f"[gpu] spmm_grad {rows}x{cols} {n} form {form} splits {splits}", flush=True)
         w, dy = _exact(rows, cols, n, sw, rows + n)
         m = spdp.encode(w, (256, 16))
         _check_exact(m, w, dy, f"{rows}x{cols} {n}")
