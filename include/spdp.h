@@ -323,8 +323,9 @@ typedef struct spdp_adapters {
  *              that receive h (0 for tokens without an adapter), which
  *              spdp_adapt_grad reads.
  *   n_tokens   1 <= n_tokens <= 2^20.
- *   workspace  device, 256-byte aligned, spdp_adapt_workspace bytes, the call's
- *              alone until the stream has passed it; it overlaps no other array.
+ *   workspace  device, 256-byte aligned, spdp_adapt_workspace bytes (which may
+ *              be 0: then NULL will do), the call's alone until the stream has
+ *              passed it; it overlaps no other array.
  *   stream     hipStream_t to enqueue on (of the current device, which all
  *              arrays are on).
  *

@@ -195,23 +195,26 @@ def _ptr(a: np.ndarray) -> ctypes.c_void_p:
 def _tensor(t, name: str, dtype, shape) -> None:
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} tensor")
 
 
-def _stream(stream, *tensors):
+def _stream(stream, tensors) -> int:
     """The HIP stream to enqueue on, after a check of the tensors' device."""
     import torch
-    dev = tensors[0].device
+    dev = tensors[0].get_device()  # -1: not on a GPU
     for t in tensors:
-        if not t.is_cuda or t.device != dev:
+        if t.get_device() != dev or dev < 0:
             raise ValueError("all tensors must be on one GPU")
-    if torch.cuda.current_device() != dev.index:
+    if torch.cuda.current_device() != dev:
         raise ValueError("the tensors are not on the current device")
-    s = stream if stream is not None else torch.cuda.current_stream(dev)
-    if s.device != dev:
+    if stream is None:
+        # (the stream's number alone: an object of it takes longer than a launch)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
+    if stream.device.index != dev:
         raise ValueError("the stream is not on the tensors' device")
-    return s.cuda_stream
+    return stream.cuda_stream
 
 
 def _workspace(size: int, device, stream):
@@ -220,9 +223,9 @@ def _workspace(size: int, device, stream):
     only to work behind the call."""
     import torch
     if stream is None:
-        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+        return torch.empty(size or 1, dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+        return torch.empty(size or 1, dtype=torch.uint8, device=device)
 
 
 class Matrix:
@@ -361,7 +364,7 @@ class Matrix:
         n = dy.shape[0]
         _tensor(dy, "dy", torch.float16, (n, self.rows))
         _tensor(dx, "dx", torch.float16, (n, self.cols))
-        s = _stream(stream, dy, dx)
+        s = _stream(stream, (dy, dx))
         need = ctypes.c_size_t()
         _check(lib().spdp_spmm_grad_workspace(self._h, n, ctypes.byref(need)))
         ws = _workspace(need.value, dy.device, stream)
@@ -498,10 +501,11 @@ class Adapters:
         _tensor(a, "a", torch.float16, (count, rank, cols))
         _tensor(b, "b", torch.float16, (count, rank, b.shape[2]))
         _tensor(scale, "scale", torch.float32, (count,))
-        _stream(None, a, b, scale)
+        _stream(None, (a, b, scale))
         self.a, self.b, self.scale = a, b, scale
         self.count, self.rank, self.rows, self.cols = count, rank, b.shape[2], cols
         self._bank = _Bank(a.data_ptr(), b.data_ptr(), scale.data_ptr(), self.rows, cols, count, rank)
+        self._sizes = {}  # workspaces of calls, by their sizes
         need = ctypes.c_size_t()  # checks the sizes
         _check(lib().spdp_adapt_workspace(ctypes.byref(self._bank), 1, 1, 0, ctypes.byref(need)))
 
@@ -540,7 +544,7 @@ class Adapters:
         if ids is not None:
             _tensor(ids, "ids", torch.int32, (n,))
             some += (ids,)
-        s = _stream(stream, *some)
+        s = _stream(stream, some)
         need = ctypes.c_size_t()
         bank = ctypes.byref(self._bank)
         _check(lib().spdp_adapt_grad_workspace(bank, n, ids is not None, ctypes.byref(need)))
@@ -558,28 +562,38 @@ def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
     k = len(banks)
     if not (len(xs) == len(bases) == len(ys) == k) or (hs is not None and len(hs) != k) or k == 0:
         raise ValueError("banks, xs, bases, ys and hs must have one entry per projection")
-    n = xs[0].shape[0]
-    some = []
-    for i, (m, x, base, y) in enumerate(zip(banks, xs, bases, ys)):
-        _tensor(x, "x", torch.float16, (n, m.cols))
-        _tensor(base, "base", torch.float16, (n, m.rows))
-        _tensor(y, "y", torch.float16, (n, m.rows))
-        some += (x, base, y, m.a)
-        if hs is not None:
-            _tensor(hs[i], "h", torch.float32, (n, m.rank))
-            some.append(hs[i])
+    f16, n, L = torch.float16, xs[0].shape[0], lib()
+    some = [m.a for m in banks]
+    some += xs
+    some += bases
+    some += ys
+    for m, x, base, y in zip(banks, xs, bases, ys):
+        _tensor(x, "x", f16, (n, m.cols))
+        _tensor(base, "base", f16, (n, m.rows))
+        _tensor(y, "y", f16, (n, m.rows))
+    if hs is not None:
+        for m, h in zip(banks, hs):
+            _tensor(h, "h", torch.float32, (n, m.rank))
+        some += hs
     if ids is not None:
         _tensor(ids, "ids", torch.int32, (n,))
         some.append(ids)
-    s = _stream(stream, *some)
+    s = _stream(stream, some)
     P = ctypes.c_void_p * k
     bk = (_Bank * k)(*[m._bank for m in banks])
-    need = ctypes.c_size_t()
-    _check(lib().spdp_adapt_workspace(bk, k, n, ids is not None, ctypes.byref(need)))
-    ws = _workspace(need.value, xs[0].device, stream)
-    _check(lib().spdp_adapt(bk, k, P(*[x.data_ptr() for x in xs]), None if ids is None else ids.data_ptr(),
-                            P(*[b.data_ptr() for b in bases]), P(*[y.data_ptr() for y in ys]),
-                            None if hs is None else P(*[h.data_ptr() for h in hs]), n, ws.data_ptr(), need.value, s))
+    # the size of a workspace depends on nothing but the call's sizes
+    key = (n, ids is not None, tuple((m.rows, m.cols, m.rank, m.count) for m in banks[1:]))
+    size = banks[0]._sizes.get(key)
+    if size is None:
+        need = ctypes.c_size_t()
+        _check(L.spdp_adapt_workspace(bk, k, n, ids is not None, ctypes.byref(need)))
+        if len(banks[0]._sizes) >= 256:
+            banks[0]._sizes.clear()
+        banks[0]._sizes[key] = size = need.value
+    ws = _workspace(size, xs[0].device, stream)
+    _check(L.spdp_adapt(bk, k, P(*[x.data_ptr() for x in xs]), None if ids is None else ids.data_ptr(),
+                        P(*[b.data_ptr() for b in bases]), P(*[y.data_ptr() for y in ys]),
+                        None if hs is None else P(*[h.data_ptr() for h in hs]), n, ws.data_ptr(), size, s))
 
 
 def _heads(xs, dim, pos, cos, sin, ys, weights, eps, interleaved, stream, dys=None, dweights=None):
@@ -589,40 +603,40 @@ def _heads(xs, dim, pos, cos, sin, ys, weights, eps, interleaved, stream, dys=No
         raise ValueError("every list must have one entry per input")
     if dim < 1:
         raise ValueError("dim must be at least 1")
-    n = xs[0].shape[0]
+    f16, n = torch.float16, xs[0].shape[0]
     _tensor(pos, "pos", torch.int32, (n,))
     if cos.dim() != 2:
         raise ValueError("cos and sin must be [positions, rot / 2]")
     _tensor(cos, "cos", torch.float32, cos.shape)
     _tensor(sin, "sin", torch.float32, cos.shape)
-    some = [xs[0], pos, cos, sin]
-    inputs = (_Heads * k)()
+    some = [pos, cos, sin]
+    some += xs
+    some += ys
+    inputs = []
     for i, (x, y) in enumerate(zip(xs, ys)):
         if x.dim() != 2 or x.shape[1] % dim or x.shape[1] == 0:
             raise ValueError(f"x must be [tokens, heads * {dim}]")
-        _tensor(x, "x", torch.float16, (n, x.shape[1]))
-        _tensor(y, "the output", torch.float16, x.shape)
-        some += (x, y)
-        m = inputs[i]
-        m.x, m.y, m.heads = x.data_ptr(), y.data_ptr(), x.shape[1] // dim
-        w = None if weights is None else weights[i]
-        if w is not None:
-            _tensor(w, "a weight", torch.float16, (dim,))
-            some.append(w)
-            m.weight = w.data_ptr()
+        width = x.shape[1]
+        _tensor(x, "x", f16, (n, width))
+        _tensor(y, "the output", f16, (n, width))
+        w = d = dw = None
+        if weights is not None and weights[i] is not None:
+            _tensor(weights[i], "a weight", f16, (dim,))
+            some.append(weights[i])
+            w = weights[i].data_ptr()
         if dys is not None:
-            _tensor(dys[i], "dy", torch.float16, x.shape)
+            _tensor(dys[i], "dy", f16, (n, width))
             some.append(dys[i])
-            m.dy = dys[i].data_ptr()
-        d = None if dweights is None else dweights[i]
-        if d is not None:
-            _tensor(d, "a weight's gradient", torch.float32, (dim,))
-            some.append(d)
-            m.dweight = d.data_ptr()
-    s = _stream(stream, *some)
-    r = _Rotation(pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), cos.shape[0], dim, 2 * cos.shape[1],
-                  int(bool(interleaved)), eps)
-    return inputs, k, ctypes.byref(r), n, s
+            d = dys[i].data_ptr()
+        if dweights is not None and dweights[i] is not None:
+            _tensor(dweights[i], "a weight's gradient", torch.float32, (dim,))
+            some.append(dweights[i])
+            dw = dweights[i].data_ptr()
+        inputs.append(_Heads(x.data_ptr(), w, d, y.data_ptr(), dw, width // dim))
+    s = _stream(stream, some)
+    table, half = cos.shape
+    r = _Rotation(pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), table, dim, 2 * half, 1 if interleaved else 0, eps)
+    return (_Heads * k)(*inputs), k, ctypes.byref(r), n, s
 
 
 def rotate_heads(xs, dim, pos, cos, sin, ys, weights=None, eps=1e-6, interleaved=False, stream=None) -> None:

@@ -11,8 +11,8 @@
 //   outer_kernel   an adapter's sums over its tokens of h times input (the
 //                  factors' gradients), split over the tokens where the grid
 //                  is small; outer_reduce_kernel adds the splits in order.
-//   sort_kernel    tokens in the order of their adapters, and tiles of 32 of
-//                  them, so that an MFMA's tokens share a factor.
+//   sort_kernel    tokens in the order of their adapters, and tiles of them, so
+//                  that an MFMA's tokens share a factor.
 //
 // Both factors are kept rank by rank ([adapter][rank][width]): the backward
 // pass is the forward one with the factors exchanged (u = B^T dY by
@@ -41,36 +41,38 @@ using namespace spdp_dev;
 
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 32;  // tokens of a tile
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 
-// The tokens of tile `block` to tok[0 .. kTile - 1] (places past the count
-// repeat one of them); false: no tile. Every wave does it alike.
-__device__ __forceinline__ bool take_tile(const Tokens& t, int block, int* tok, int& adapter, int& count) {
+// The tokens of tile `block`, at most T, to tok[0 .. T - 1] (places past the
+// count repeat one of them); false: no tile. Every wave does it alike.
+// `subs`: T-token parts of the sort's tiles.
+template <int T>
+__device__ __forceinline__ bool take_tile(const Tokens& t, int block, int* tok, int& adapter, int& count, int subs = 1) {
   const int lane = threadIdx.x & 63;
   if (t.ids == nullptr) {
     adapter = 0;
-    count = min(kTile, t.n_tokens - block * kTile);
-    if (lane < kTile) tok[lane] = block * kTile + min(lane, count - 1);
+    count = min(T, t.n_tokens - block * T);
+    if (lane < T) tok[lane] = block * T + min(lane, count - 1);
   } else if (t.tiles == nullptr) {
-    // the tile of token `block`, which has to be the first, 33rd, ... of its adapter
+    // the tile of token `block`, which has to be the first, (T + 1)st, ... of its adapter
     int id = lane < t.n_tokens ? t.ids[lane] : -2;
     if (id >= t.count || (lane < t.n_tokens && id < 0)) id = -1;
     adapter = __builtin_amdgcn_readlane(id, block);
     const uint64_t same = __ballot(lane < t.n_tokens && id == adapter);
     const int first = __popcll(same & ((1ull << block) - 1));
-    if (first % kTile != 0) return false;
-    count = min(kTile, (int)__popcll(same) - first);
+    if (first % T != 0) return false;
+    count = min(T, (int)__popcll(same) - first);
     const int rank = (int)__popcll(same & ((1ull << lane) - 1)) - first;
-    if ((same >> lane & 1) && rank >= 0 && rank < kTile) tok[rank] = lane;
-    if (lane >= count && lane < kTile) tok[lane] = block;
+    if ((same >> lane & 1) && rank >= 0 && rank < T) tok[rank] = lane;
+    if (lane >= count && lane < T) tok[lane] = block;
   } else {
-    const Tile d = t.tiles[block];
+    const Tile d = t.tiles[block / subs];
+    const int skip = block % subs * T;
     adapter = d.adapter;
-    count = d.count;
-    if (count == 0) return false;
-    if (lane < kTile) tok[lane] = t.perm[d.start + min(lane, count - 1)];
+    count = min(T, d.count - skip);
+    if (count <= 0) return false;
+    if (lane < T) tok[lane] = t.perm[d.start + skip + min(lane, count - 1)];
   }
   wave_fence();
   return true;
@@ -78,80 +80,114 @@ __device__ __forceinline__ bool take_tile(const Tokens& t, int block, int* tok, 
 
 // ---------------------------------------------------------------------------
 // Shrink. A workgroup owns a tile of tokens and a range of the width, its four
-// waves every fourth step of 32 columns; 16x16x32 MFMAs with the tokens as
+// waves every fourth step of 64 columns; 16x16x32 MFMAs with the tokens as
 // rows. The waves' sums are added in LDS.
 
-constexpr int kStep = 32;
+constexpr int kStep = 64;
 
-template <int RB>  // 16 RB ranks
-__global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
-  __shared__ int tok[kTile];
-  extern __shared__ __attribute__((aligned(16))) float red[];  // [wave][token][16 RB]
-  const Shrink& m = a.m[blockIdx.z];
+// The sums over the steps [s0, s1) of in's rows tok[0 .. T - 1] times the
+// adapter's factor, each of W waves' share to red [wave][token][16 RB].
+template <int RB, int T, int W>
+__device__ __forceinline__ void shrink_steps(const uint16_t* in, const uint16_t* factor, int width, int rank, const int* tok,
+                                             int s0, int s1, float* red) {
+  constexpr int TB = T / 16;
+  // halves of a step that are loaded at once, the next ones during their MFMAs
+  constexpr int D = RB * TB <= 2 ? 4 : RB * TB <= 4 ? 2 : 1;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int adapter, count;
-  if (!take_tile(a.t, blockIdx.x, tok, adapter, count) || adapter < 0) return;
-  const int steps = (m.width + kStep - 1) / kStep;
-  const int s0 = (int)blockIdx.y * m.per, s1 = min(steps, s0 + m.per);
-  if (s0 >= steps) return;  // the grid has the most ranges of the launch's products
-  const int k0 = 8 * (lane >> 4);
-  const uint16_t *px[2], *pf[RB];
+  // four lanes have a row's 64 columns, 16 of them each: 128 bytes of a row at
+  // a time (in an order of the sum that both operands share)
+  const int k0 = 16 * (lane >> 4);
+  const uint16_t *px[TB], *pf[RB];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) px[i] = m.in + (size_t)tok[16 * i + (lane & 15)] * m.width + k0;
+  for (int i = 0; i < TB; ++i) px[i] = in + (size_t)tok[16 * i + (lane & 15)] * width + k0;
 #pragma unroll
-  for (int j = 0; j < RB; ++j)
-    pf[j] = m.factor + ((size_t)adapter * a.rank + min(16 * j + (lane & 15), a.rank - 1)) * m.width + k0;
+  for (int j = 0; j < RB; ++j) pf[j] = factor + (size_t)min(16 * j + (lane & 15), rank - 1) * width + k0;
 
-  float4v acc[2][RB];
+  float4v acc[TB][RB];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TB; ++i)
 #pragma unroll
     for (int j = 0; j < RB; ++j) acc[i][j] = float4v{0, 0, 0, 0};
-  const bool two = count > 16;
-  // steps whose columns all lie inside the width, kDeep of them at a time
-  constexpr int kDeep = RB == 8 ? 2 : 4;
-  const int whole = min(s1, m.width / kStep);
-  int s = s0 + wave;
-  auto multiply = [&](const half8 (&x)[2], const half8 (&f)[RB]) __attribute__((always_inline)) {
+  struct Halves {
+    half8 x[D][TB], f[D][RB];
+  };
+  // from half h of the wave on; `whole`: all columns lie inside the width
+  auto load = [&](int h, bool whole, Halves& b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < RB; ++j) {
-      acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[0], f[j], acc[0][j], 0, 0, 0);
-      if (two) acc[1][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[1], f[j], acc[1][j], 0, 0, 0);
+    for (int d = 0; d < D; ++d) {
+      const int at = (s0 + wave + ((h + d) >> 1) * W) * kStep + 8 * ((h + d) & 1);
+      const int left = whole ? 8 : max(width - at - k0, 0);
+#pragma unroll
+      for (int i = 0; i < TB; ++i) b.x[d][i] = whole ? load8(px[i] + at) : load8_inside(px[i] + at, left);
+#pragma unroll
+      for (int j = 0; j < RB; ++j) b.f[d][j] = whole ? load8(pf[j] + at) : load8_inside(pf[j] + at, left);
     }
   };
-  for (; s + (kDeep - 1) * kWaves < whole; s += kDeep * kWaves) {
-    half8 x[kDeep][2], f[kDeep][RB];
+  auto multiply = [&](const Halves& b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int d = 0; d < kDeep; ++d) {
-      const int at = (s + d * kWaves) * kStep;
-      x[d][0] = load8(px[0] + at);
-      x[d][1] = two ? load8(px[1] + at) : x[d][0];
+    for (int d = 0; d < D; ++d)
 #pragma unroll
-      for (int j = 0; j < RB; ++j) f[d][j] = load8(pf[j] + at);
-    }
+      for (int i = 0; i < TB; ++i)
 #pragma unroll
-    for (int d = 0; d < kDeep; ++d) multiply(x[d], f[d]);
+        for (int j = 0; j < RB; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b.x[d][i], b.f[d][j], acc[i][j], 0, 0, 0);
+  };
+  // the wave's halves that lie inside the width, by batches of D, then the rest
+  const int mine = max(0, (min(s1, width / kStep) - s0 - wave + W - 1) / W);
+  const int inside = 2 * mine / D;
+  Halves even, odd;
+  int b = 0;
+  if (b < inside) load(0, true, even);
+  while (b < inside) {
+    if (b + 1 < inside) load((b + 1) * D, true, odd);
+    multiply(even);
+    if (++b >= inside) break;
+    if (b + 1 < inside) load((b + 1) * D, true, even);
+    multiply(odd);
+    ++b;
   }
-  for (; s < s1; s += kWaves) {
-    const int at = s * kStep;
-    const int left = m.width - at - k0;
-    half8 x[2], f[RB];
+  // (a step past the range, or columns past the width, load zeros)
+  const int all = 2 * max(0, (s1 - s0 - wave + W - 1) / W);
+  for (int h = inside * D; h < all; h += D) {
+    if constexpr (D <= 2) {
+      load(h, false, even);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = load8_inside(px[i] + at, left);
+      for (int d = 0; d < D; ++d) {
+        const int at = (s0 + wave + ((h + d) >> 1) * W) * kStep + 8 * ((h + d) & 1);
+        const int left = h + d < all ? max(width - at - k0, 0) : 0;
 #pragma unroll
-    for (int j = 0; j < RB; ++j) f[j] = load8_inside(pf[j] + at, left);
-    multiply(x, f);
+        for (int i = 0; i < TB; ++i) even.x[d][i] = load8_inside(px[i] + at, left);
+#pragma unroll
+        for (int j = 0; j < RB; ++j) even.f[d][j] = load8_inside(pf[j] + at, left);
+      }
+    }
+    multiply(even);
   }
 
   // register e of block (i, j): token 16 i + 4 (lane / 16) + e, rank 16 j + lane mod 16
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TB; ++i)
 #pragma unroll
     for (int j = 0; j < RB; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        red[((wave * kTile + 16 * i + 4 * (lane >> 4) + e) * RB + j) * 16 + (lane & 15)] = acc[i][j][e];
+        red[((wave * T + 16 * i + 4 * (lane >> 4) + e) * RB + j) * 16 + (lane & 15)] = acc[i][j][e];
+}
+
+template <int RB, int T>  // 16 RB ranks, tiles of T tokens
+__global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
+  __shared__ int tok[T];
+  extern __shared__ __attribute__((aligned(16))) float red[];  // [wave][token][16 RB]
+  const Shrink& m = a.m[blockIdx.z];
+  int adapter, count;
+  if (!take_tile<T>(a.t, blockIdx.x, tok, adapter, count) || adapter < 0) return;
+  const int steps = (m.width + kStep - 1) / kStep;
+  const int s0 = (int)blockIdx.y * m.per;
+  if (s0 >= steps) return;  // the grid has the most ranges of the launch's products
+  shrink_steps<RB, T, kWaves>(m.in, m.factor + (size_t)adapter * a.rank * m.width, m.width, a.rank, tok, s0,
+                              min(steps, s0 + m.per), red);
   __syncthreads();
   float* const part = m.part + (size_t)blockIdx.y * a.t.n_tokens * a.rank;
   for (int q = threadIdx.x; q < count * 16 * RB; q += kThreads) {
@@ -159,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
     if (j >= a.rank) continue;
     float sum = red[q];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum += red[w * kTile * 16 * RB + q];
+    for (int w = 1; w < kWaves; ++w) sum += red[w * T * 16 * RB + q];
     part[(size_t)tok[t] * a.rank + j] = sum;
   }
 }
@@ -190,89 +226,167 @@ __device__ __forceinline__ void split2(float v, _Float16& hi, _Float16& lo) {
 // that base and output are read and written 128 bytes of a token at a time.
 
 constexpr int kCols = 64;        // columns of a wave
-constexpr int kBlock = kCols * kWaves;
 constexpr int kFactorRow = 144;  // bytes of a factor row in LDS: 64 fp16 + 16, which spreads the rows over the banks
 constexpr int kOutRow = 72;      // floats of a row of sums
 
-template <int RB>
+//
+// Few tokens and a small first factor: the fused form of eight waves computes h
+// as well, every workgroup for itself, while its base and factor are on their
+// way; one launch instead of two.
+
+constexpr int kFusedWaves = 8;
+
+template <int RB, int T, int W>
 struct ExpandCfg {
   static constexpr int kRank = 16 * RB;
   static constexpr int kActRow = 2 * kRank + 16;  // bytes
-  static constexpr int kWave = kRank * kFactorRow > 4 * kTile * kOutRow ? kRank * kFactorRow : 4 * kTile * kOutRow;
-  static constexpr int kLds = 2 * kTile * kActRow + kWaves * kWave;
+  static constexpr int kWave = kRank * kFactorRow > 4 * T * kOutRow ? kRank * kFactorRow : 4 * T * kOutRow;
+  static constexpr int kActs = 32 * kActRow;  // (an MFMA reads 32 rows)
+  static constexpr int kLds = 2 * kActs + W * kWave;
+  static_assert(W * T * kRank * 4 <= W * kWave, "the waves' shares of h fit");
 };
 
-template <int RB>
-__global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a) {
-  using C = ExpandCfg<RB>;
-  __shared__ int tok[kTile];
-  __shared__ float mult[kTile];
+template <int RB, int T, bool FUSED>  // 16 RB ranks, tiles of T <= 32 tokens
+__global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_kernel(ExpandArgs a) {
+  constexpr int W = FUSED ? kFusedWaves : kWaves;
+  constexpr int kBlock = kCols * W;
+  using C = ExpandCfg<RB, T, W>;
+  constexpr int kPasses = T / 8;  // of 8 tokens x 64 columns
+  __shared__ int tok[T];
+  __shared__ float mult[T];
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const Expand& m = a.m[blockIdx.z];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if ((int)blockIdx.x * a.blocks * kBlock >= m.width) return;
+  if ((int)blockIdx.x * kBlock >= m.width) return;
   int adapter, count;
-  if (!take_tile(a.t, blockIdx.y, tok, adapter, count)) return;
+  if (!take_tile<T>(a.t, blockIdx.y, tok, adapter, count, a.subs)) return;
   unsigned char* const act_hi = lds;
-  unsigned char* const act_lo = lds + kTile * C::kActRow;
-  unsigned char* const mine = lds + 2 * kTile * C::kActRow + wave * C::kWave;
+  unsigned char* const act_lo = lds + C::kActs;
+  unsigned char* const mine = lds + 2 * C::kActs + wave * C::kWave;
+  // neighbouring workgroups have neighbouring blocks at a time
+  const int first = (int)blockIdx.x * kBlock + wave * kCols + 8 * (lane & 7);
+  const int stride = (int)gridDim.x * kBlock;
+  const uint16_t* const factor = m.factor + (size_t)max(adapter, 0) * a.rank * m.width;
+  size_t row[kPasses];  // of the lane's tokens
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) row[p] = (size_t)tok[8 * p + (lane >> 3)] * m.width;
 
-  if (adapter >= 0) {
-    // eight threads a token
-    const int t = threadIdx.x >> 3;
-    const size_t row = (size_t)tok[t] * a.rank;
-    const size_t plane = (size_t)a.t.n_tokens * a.rank;
-    float v[2 * RB];
-    float largest = 0.0f;
+  // a block's base and factor, requested a block ahead
+  half8 base[kPasses], fac[2 * RB];
+  auto request = [&](int col) __attribute__((always_inline)) {
+    const int left = m.width - col;  // columns of the lane's eight that there are; may be negative
+    if (left <= 0) return;
 #pragma unroll
-    for (int i = 0; i < 2 * RB; ++i) {
-      const int j = 8 * i + (threadIdx.x & 7);
-      v[i] = 0.0f;
-      if (j < a.rank)
-        for (int s = 0; s < m.splits; ++s) v[i] += m.part[s * plane + row + j];
-      if (m.keep != nullptr && blockIdx.x == 0 && t < count && j < a.rank) m.keep[row + j] = v[i];
-      largest = fmaxf(largest, finite_abs(v[i]));
+    for (int p = 0; p < kPasses; ++p)
+      if (8 * p + (lane >> 3) < count) base[p] = load8_inside(m.base + row[p] + col, left);
+    if (adapter < 0) return;
+#pragma unroll
+    for (int p = 0; p < 2 * RB; ++p) {
+      const int j = 8 * p + (lane >> 3);
+      if (j < a.rank) fac[p] = load8_inside(factor + (size_t)j * m.width + col, left);
     }
+  };
+  const half8 none = half8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int d = 1; d < 8; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
-    float up, down;
-    pick_scale(largest, up, down);
+  for (int p = 0; p < kPasses; ++p) base[p] = none;
 #pragma unroll
-    for (int i = 0; i < 2 * RB; ++i) {
-      _Float16 hi, lo;
-      split2(v[i] * up, hi, lo);
-      const int at = t * C::kActRow + 2 * (8 * i + (threadIdx.x & 7));
-      *reinterpret_cast<_Float16*>(act_hi + at) = hi;
-      *reinterpret_cast<_Float16*>(act_lo + at) = lo;
+  for (int p = 0; p < 2 * RB; ++p) fac[p] = none;
+  request(first);
+
+  float* const red = reinterpret_cast<float*>(lds + 2 * C::kActs);
+  if constexpr (FUSED) {
+    if (adapter >= 0)
+      shrink_steps<RB, T, W>(m.in, m.first_factor + (size_t)adapter * a.rank * m.in_width, m.in_width, a.rank, tok, 0,
+                             (m.in_width + kStep - 1) / kStep, red);
+    __syncthreads();
+  }
+  const int part8 = threadIdx.x & 7;  // eight threads a token
+  const bool lead = blockIdx.x == 0;
+  const int t = threadIdx.x >> 3;
+  if (t < T) {
+    const size_t at0 = (size_t)tok[t] * a.rank;
+    if (adapter >= 0) {
+      const size_t plane = (size_t)a.t.n_tokens * a.rank;
+      float v[2 * RB];
+      float largest = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 2 * RB; ++i) v[i] = 0.0f;
+      if constexpr (FUSED) {
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+          for (int i = 0; i < 2 * RB; ++i) v[i] += red[(w * T + t) * C::kRank + 8 * i + part8];
+#pragma unroll
+        for (int i = 0; i < 2 * RB; ++i)  // (ranks that are none repeat the last)
+          if (8 * i + part8 >= a.rank) v[i] = 0.0f;
+      } else {
+        // all ranks of four ranges in flight, added in order
+        for (int s0 = 0; s0 < m.splits; s0 += 4) {
+          float x[4][2 * RB];
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < 2 * RB; ++i) {
+              const int j = 8 * i + part8;
+              x[s][i] = s0 + s < m.splits && j < a.rank ? m.part[(s0 + s) * plane + at0 + j] : 0.0f;
+            }
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < 2 * RB; ++i) v[i] += x[s][i];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * RB; ++i) {
+        const int j = 8 * i + part8;
+        if (m.keep != nullptr && lead && t < count && j < a.rank) m.keep[at0 + j] = v[i];
+        largest = fmaxf(largest, finite_abs(v[i]));
+      }
+#pragma unroll
+      for (int d = 1; d < 8; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
+      float up, down;
+      pick_scale(largest, up, down);
+#pragma unroll
+      for (int i = 0; i < 2 * RB; ++i) {
+        _Float16 hi, lo;
+        split2(v[i] * up, hi, lo);
+        const int at = t * C::kActRow + 2 * (8 * i + part8);
+        *reinterpret_cast<_Float16*>(act_hi + at) = hi;
+        *reinterpret_cast<_Float16*>(act_lo + at) = lo;
+      }
+      if (part8 == 0) {
+        mult[t] = down * m.scale[adapter];
+        if (m.most != nullptr && lead && t < count) m.most[tok[t]] = largest;
+      }
+      if (m.most != nullptr && lead && t < count) {
+        float other = 0.0f;
+        for (int j = part8; j < a.rank; j += 8) other = fmaxf(other, finite_abs(m.other[at0 + j]));
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) other = fmaxf(other, __shfl_xor(other, d));
+        if (part8 == 0) m.most[a.t.n_tokens + tok[t]] = other;
+      }
+    } else if (m.keep != nullptr && lead && t < count) {
+      for (int j = part8; j < a.rank; j += 8) m.keep[at0 + j] = 0.0f;
     }
-    if ((threadIdx.x & 7) == 0) mult[t] = down * m.scale[adapter];
-  } else if (m.keep != nullptr && blockIdx.x == 0) {
-    for (int q = threadIdx.x; q < count * a.rank; q += kThreads)
-      m.keep[(size_t)tok[q / a.rank] * a.rank + q % a.rank] = 0.0f;
   }
   __syncthreads();
 
   for (int b = 0; b < a.blocks; ++b) {
-    const int n0 = ((int)blockIdx.x * a.blocks + b) * kBlock + wave * kCols;
-    if (n0 >= m.width) return;
-    const int col = n0 + 8 * (lane & 7);
-    const int left = m.width - col;  // columns of the lane's eight that there are; may be negative
-    half8 base[4];
+    const int col = first + b * stride;
+    if (col - 8 * (lane & 7) >= m.width) return;
+    const int left = m.width - col;
+    half8 mybase[kPasses];
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int t = 8 * p + (lane >> 3);
-      if (t < count && left > 0) base[p] = load8_inside(m.base + (size_t)tok[t] * m.width + col, left);
-    }
+    for (int p = 0; p < kPasses; ++p) mybase[p] = base[p];
     if (adapter >= 0) {
-      const uint16_t* const f = m.factor + (size_t)adapter * a.rank * m.width + col;
 #pragma unroll
-      for (int p = 0; p < 2 * RB; ++p) {
-        const int j = 8 * p + (lane >> 3);
-        half8 v = half8{0, 0, 0, 0, 0, 0, 0, 0};
-        if (j < a.rank && left > 0) v = load8_inside(f + (size_t)j * m.width, left);
-        *reinterpret_cast<half8*>(mine + j * kFactorRow + 16 * (lane & 7)) = v;
-      }
+      for (int p = 0; p < 2 * RB; ++p)
+        *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = left > 0 ? fac[p] : none;
+    }
+    if (b + 1 < a.blocks) request(col + stride);
+    float* const sums = reinterpret_cast<float*>(mine);
+    if (adapter >= 0) {
       wave_fence();
       float16v acc[2] = {float16v{}, float16v{}};
 #pragma unroll
@@ -288,26 +402,25 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a) {
       }
       wave_fence();
       // register e: token 8 (e / 4) + 4 (lane / 32) + e mod 4, column lane mod 32
-      float* const sums = reinterpret_cast<float*>(mine);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
+        for (int e = 0; e < T / 2; ++e)
           sums[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * kOutRow + 32 * i + (lane & 31)] = acc[i][e];
       wave_fence();
     }
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int t = 8 * p + (lane >> 3);
-      if (t >= count || left <= 0) continue;
-      half8 y = base[p];
+    for (int p = 0; p < kPasses; ++p) {
+      const int q = 8 * p + (lane >> 3);
+      if (q >= count || left <= 0) continue;
+      half8 y = mybase[p];
       if (adapter >= 0) {
-        const float* const sums = reinterpret_cast<const float*>(mine) + t * kOutRow + 8 * (lane & 7);
-        const float by = mult[t];
+        const float* const sum = sums + q * kOutRow + 8 * (lane & 7);
+        const float by = mult[q];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (_Float16)__fmaf_rn(by, sums[e], (float)base[p][e]);
+        for (int e = 0; e < 8; ++e) y[e] = (_Float16)__fmaf_rn(by, sum[e], (float)mybase[p][e]);
       }
-      store8_inside(m.out + (size_t)tok[t] * m.width + col, y, left);
+      store8_inside(m.out + row[p] + col, y, left);
     }
     wave_fence();
   }
@@ -315,45 +428,87 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(ExpandArgs a) {
 
 // ---------------------------------------------------------------------------
 // Outer: for an adapter, out[j][f] = scale * sum over its tokens of act[t][j]
-// in[t][f]. A workgroup owns 64 columns, all ranks and a range of the tokens,
-// each wave every fourth group of 16 tokens (an MFMA's k); the input goes
-// through the wave's LDS and transposing reads, and the waves' sums are added
-// in LDS at the end.
+// in[t][f]. A piece is an adapter's tokens or, split, a part of them.
+//
+// pack_kernel lays a piece's activations out as the MFMA's operands, scaled by
+// one power of two (by each token's largest, which expand_kernel has left) and
+// split into two fp16: [group of 16 tokens][block of 32
+// ranks][high, low][lane][8]. outer_kernel's workgroup owns 64 columns, all
+// ranks and a piece, each wave every fourth group (an MFMA's k); the input goes
+// through the wave's LDS and transposing reads, one group ahead, and the waves'
+// sums are added in LDS at the end.
 
 constexpr int kGroup = 16;  // tokens of an MFMA
+
+struct Piece {
+  int t0, t1;        // in perm
+  long long group0;  // of the packed groups: those of pieces before it are fewer
+  int index;
+};
+__device__ __forceinline__ Piece piece_of(const OuterArgs& a, int adapter, int split) {
+  const int b0 = a.first ? a.first[adapter] : 0;
+  const int b1 = a.first ? a.first[adapter + 1] : adapter == 0 ? a.n_tokens : 0;
+  const int per = ((b1 - b0 + a.splits - 1) / a.splits + kGroup - 1) / kGroup * kGroup;
+  Piece p;
+  p.t0 = min(b1, b0 + split * per);
+  p.t1 = min(b1, p.t0 + per);
+  p.index = adapter * a.splits + split;
+  p.group0 = p.t0 / kGroup + p.index;
+  return p;
+}
+
+template <int RB>  // 32 RB ranks
+__global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
+  __shared__ float all[kWaves];
+  const int which = (int)blockIdx.z / a.count, adapter = (int)blockIdx.z % a.count;
+  const Outer& m = a.m[which];
+  const Piece p = piece_of(a, adapter, blockIdx.y);
+  const int n = p.t1 - p.t0;
+  float largest = 0.0f;
+#pragma unroll 4
+  for (int q = threadIdx.x; q < n; q += kThreads)
+    largest = fmaxf(largest, m.most[a.perm ? a.perm[p.t0 + q] : p.t0 + q]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
+  if ((threadIdx.x & 63) == 0) all[threadIdx.x >> 6] = largest;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, all[w]);
+  float up, down;
+  pick_scale(largest, up, down);
+  if (threadIdx.x == 0 && blockIdx.x == 0) m.down[p.index] = down;
+  // one lane's operand at a time
+  const int groups = (n + kGroup - 1) / kGroup;
+  for (int q = (int)blockIdx.x * kThreads + threadIdx.x; q < groups * RB * 64; q += (int)gridDim.x * kThreads) {
+    const int lane = q & 63, block = (q >> 6) % RB, g = (q >> 6) / RB;
+    const int j = 32 * block + (lane & 31);
+    half8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int t = p.t0 + g * kGroup + 8 * (lane >> 5) + e;
+      _Float16 h, l;
+      split2(t < p.t1 && j < a.rank ? m.act[(size_t)(a.perm ? a.perm[t] : t) * a.rank + j] * up : 0.0f, h, l);
+      hi[e] = h;
+      lo[e] = l;
+    }
+    half8* const to = reinterpret_cast<half8*>(m.packed) + ((p.group0 + g) * RB + block) * 128 + lane;
+    to[0] = hi;
+    to[64] = lo;
+  }
+}
 
 template <int RB>  // 32 RB ranks
 __global__ __launch_bounds__(kThreads) void outer_kernel(OuterArgs a) {
   constexpr int kRed = 4 * kWaves * 2 * 16 * 64;
   constexpr int kIn = kWaves * kGroup * kFactorRow;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kRed > kIn ? kRed : kIn];
-  __shared__ float most[kWaves];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int which = (int)blockIdx.z / a.count, adapter = (int)blockIdx.z % a.count;
   const Outer& m = a.m[which];
   const int f0 = (int)blockIdx.x * kCols;
   if (f0 >= m.width) return;
-  int t0 = a.first ? a.first[adapter] : 0;
-  int t1 = a.first ? a.first[adapter + 1] : adapter == 0 ? a.n_tokens : 0;
-  const int per = ((t1 - t0 + a.splits - 1) / a.splits + kGroup - 1) / kGroup * kGroup;
-  t0 = min(t1, t0 + (int)blockIdx.y * per);
-  t1 = min(t1, t0 + per);
-
-  float largest = 0.0f;
-  for (int q = threadIdx.x; q < (t1 - t0) * a.rank; q += kThreads) {
-    const int p = t0 + q / a.rank;
-    const int t = a.perm ? a.perm[p] : p;
-    largest = fmaxf(largest, finite_abs(m.act[(size_t)t * a.rank + q % a.rank]));
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
-  if (lane == 0) most[wave] = largest;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) largest = fmaxf(largest, most[w]);
-  float up, down;
-  pick_scale(largest, up, down);
+  const Piece piece = piece_of(a, adapter, blockIdx.y);
 
   float16v acc[RB][2];
 #pragma unroll
@@ -361,27 +516,45 @@ __global__ __launch_bounds__(kThreads) void outer_kernel(OuterArgs a) {
   unsigned char* const mine = lds + wave * kGroup * kFactorRow;
   const int col = f0 + 8 * (lane & 7);
   const int left = m.width - col;
-  for (int g = t0 + wave * kGroup; g < t1; g += kWaves * kGroup) {
+  const half8* const packed = reinterpret_cast<const half8*>(m.packed) + piece.group0 * RB * 128 + lane;
+  const int groups = (piece.t1 - piece.t0 + kGroup - 1) / kGroup;
+  const half8 none = half8{0, 0, 0, 0, 0, 0, 0, 0};
+
+  // a group's input and operands, requested a group ahead, its tokens' places
+  // two ahead
+  int at[2];
+  half8 in[2], act[2 * RB];
+  auto places = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      const int at = g + 8 * p + (lane >> 3);
-      half8 v = half8{0, 0, 0, 0, 0, 0, 0, 0};
-      if (at < t1 && left > 0) v = load8_inside(m.in + (size_t)(a.perm ? a.perm[at] : at) * m.width + col, left);
-      *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = v;
+      const int t = piece.t0 + g * kGroup + 8 * p + (lane >> 3);
+      at[p] = t < piece.t1 ? (a.perm ? a.perm[t] : t) : -1;
     }
-    half8 hi[RB], lo[RB];
+  };
+  auto request = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int at = g + 8 * (lane >> 5) + e;
-      const float* const act = m.act + (size_t)(at < t1 ? (a.perm ? a.perm[at] : at) : 0) * a.rank;
+    for (int p = 0; p < 2; ++p) {
+      in[p] = none;
+      if (at[p] >= 0 && left > 0) in[p] = load8_inside(m.in + (size_t)at[p] * m.width + col, left);
+    }
 #pragma unroll
-      for (int j = 0; j < RB; ++j) {
-        const int r = 32 * j + (lane & 31);
-        _Float16 h, l;
-        split2(at < t1 && r < a.rank ? act[r] * up : 0.0f, h, l);
-        hi[j][e] = h;
-        lo[j][e] = l;
-      }
+    for (int j = 0; j < 2 * RB; ++j) act[j] = packed[(size_t)g * RB * 128 + 64 * j];
+  };
+  int g = wave;
+  if (g < groups) {
+    places(g);
+    request(g);
+    places(g + kWaves);
+  }
+  for (; g < groups; g += kWaves) {
+    half8 now[2 * RB];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = in[p];
+#pragma unroll
+    for (int j = 0; j < 2 * RB; ++j) now[j] = act[j];
+    if (g + kWaves < groups) {
+      request(g + kWaves);
+      places(g + 2 * kWaves);
     }
     wave_fence();
 #pragma unroll
@@ -389,14 +562,14 @@ __global__ __launch_bounds__(kThreads) void outer_kernel(OuterArgs a) {
       const half8 v = read_transposed(mine, kFactorRow, 0, 32 * i);
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
-        acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[j], v, acc[j][i], 0, 0, 0);
-        acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo[j], v, acc[j][i], 0, 0, 0);
+        acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[2 * j], v, acc[j][i], 0, 0, 0);
+        acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[2 * j + 1], v, acc[j][i], 0, 0, 0);
       }
     }
     wave_fence();
   }
 
-  const float by = down * a.scale[adapter];
+  const float by = m.down[piece.index] * a.scale[adapter];
   float* const red = reinterpret_cast<float*>(lds);  // [wave][column block][register][lane]
   float* const out = m.out + ((size_t)blockIdx.y * a.count + adapter) * a.rank * m.width;
 #pragma unroll
@@ -450,7 +623,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
 
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int* ids, int n, int count, int* perm, int* first,
-                                                            Tile* tiles, int max_tiles) {
+                                                            Tile* tiles, int max_tiles, int per_tile) {
   extern __shared__ int cnt[];  // [wave][bucket], then [bucket] first token and [bucket] first tile
   __shared__ int sums[2][kSortWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -481,7 +654,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int* ids, int 
     base[b] = tokens;
     tile0[b] = n_tiles;
     tokens += sum;
-    n_tiles += (sum + kTile - 1) / kTile;
+    n_tiles += (sum + per_tile - 1) / per_tile;
   }
   int st = tokens, sl = n_tiles;
 #pragma unroll
@@ -514,9 +687,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int* ids, int 
   __syncthreads();
   for (int b = wave; b < buckets; b += kSortWaves) {
     const int end = b + 1 < buckets ? base[b + 1] : n;
-    const int of = (end - base[b] + kTile - 1) / kTile;
+    const int of = (end - base[b] + per_tile - 1) / per_tile;
     for (int q = lane; q < of; q += 64)
-      tiles[tile0[b] + q] = Tile{b < count ? b : -1, base[b] + q * kTile, min(kTile, end - base[b] - q * kTile), 0};
+      tiles[tile0[b] + q] = Tile{b < count ? b : -1, base[b] + q * per_tile, min(per_tile, end - base[b] - q * per_tile), 0};
   }
   for (int q = all_tiles + threadIdx.x; q < max_tiles; q += kSortThreads) tiles[q] = Tile{-1, 0, 0, 0};
   int bits = 0;
@@ -562,38 +735,51 @@ int compute_units(int* cus) {
   return SPDP_OK;
 }
 
-// The ranges of the width that shrink_kernel's workgroups take: about two
-// workgroups per CU, at least 16 steps each (four per wave).
+// The ranges of the width that shrink_kernel's workgroups take: one workgroup
+// per CU, at least four steps each (one per wave), at most eight ranges, for
+// expand_kernel's workgroups all add them (4096 tokens of rank 64, 13824 wide,
+// with 2 / 4 / 8 / 16 ranges: 53 / 32 / 33 / 37 us; 4096 wide behind 1000
+// tokens the other product takes 10 us with 4 ranges and 15 with 16).
 struct Ranges {
   int per, splits;
 };
 Ranges shrink_ranges(int64_t width, long long tiles, int banks, int cus) {
   const int steps = (int)((width + kStep - 1) / kStep);
-  const int most = std::max(1, std::min(16, steps / 16));
-  const int want = (int)std::min<long long>(most, std::max<long long>(1, 2 * cus / (tiles * banks)));
+  const int most = std::max(1, std::min(8, steps / 4));
+  const int want = (int)std::min<long long>(most, (cus + tiles * banks - 1) / (tiles * banks));
   const int per = (steps + want - 1) / want;
   return {per, (steps + per - 1) / per};
 }
 
-// The token pieces of outer_kernel, about two workgroups per CU, at least 64
-// tokens each.
+// The pieces that an adapter's tokens are split into: four workgroups of
+// outer_kernel per CU (of three that a CU holds), at least 128 tokens each.
 int outer_splits(const spdp_adapters_t* m, long long n_tokens, int cus) {
   const long long wgs = ((m->rows + kCols - 1) / kCols + (m->cols + kCols - 1) / kCols) * m->count;
-  const long long want = std::max<long long>(1, 2 * cus / wgs);
-  return (int)std::min<long long>({want, 16, std::max<long long>(1, n_tokens / m->count / 64)});
+  const long long want = std::max<long long>(1, 4 * cus / wgs);
+  return (int)std::min<long long>({want, 16, std::max<long long>(1, n_tokens / m->count / 128)});
+}
+// and their packed activations: the groups of 16 tokens, one more per piece
+size_t packed_bytes(const spdp_adapters_t* m, long long n_tokens, int splits) {
+  const size_t block = m->rank <= 32 ? 1 : m->rank <= 64 ? 2 : 4;
+  return aligned(((size_t)n_tokens / kGroup + (size_t)m->count * splits + 1) * block * 2 * 64 * 16);
 }
 
 // What the sort writes, and where, and the launch's tiles.
 struct SortPlan {
   bool sorted;
+  int tile;         // tokens of a tile
   long long tiles;  // of the grid
   size_t bytes;     // perm, first, tiles
 };
-SortPlan plan_sort(long long n_tokens, int count, bool ids, bool always) {
+SortPlan plan_sort(long long n_tokens, int count, int banks, bool ids, bool always, int cus) {
   SortPlan p;
   p.sorted = ids && (always || n_tokens > kSmall);
-  p.tiles = !ids ? (n_tokens + kTile - 1) / kTile
-            : p.sorted ? n_tokens / kTile + std::min<long long>(count + 1, n_tokens) + 1
+  // larger tiles read the factors less often; smaller ones make more workgroups
+  // where there are few tokens, and waste less where an adapter has few
+  const long long own = ids ? n_tokens / std::min<long long>(count, n_tokens) : n_tokens;
+  p.tile = own >= 128 && n_tokens * banks >= 8ll * cus ? 64 : own >= 24 ? 32 : 16;
+  p.tiles = !ids ? (n_tokens + p.tile - 1) / p.tile
+            : p.sorted ? n_tokens / p.tile + std::min<long long>(count + 1, n_tokens) + 1
                        : n_tokens;
   p.bytes = p.sorted ? aligned((size_t)n_tokens * 4) + aligned((size_t)(count + 2) * 4) + aligned((size_t)p.tiles * sizeof(Tile)) : 0;
   return p;
@@ -635,7 +821,8 @@ int sort_tokens(const int32_t* ids, long long n, int count, const SortPlan& p, u
         hipFuncSetAttribute(reinterpret_cast<const void*>(sort_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute");
   }
-  hipLaunchKernelGGL(sort_kernel, dim3(1), dim3(kSortThreads), lds, st, ids, (int)n, count, perm, *first, tiles, (int)p.tiles);
+  hipLaunchKernelGGL(sort_kernel, dim3(1), dim3(kSortThreads), lds, st, ids, (int)n, count, perm, *first, tiles,
+                     (int)p.tiles, p.tile);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   t->perm = perm;
@@ -643,52 +830,86 @@ int sort_tokens(const int32_t* ids, long long n, int count, const SortPlan& p, u
   return SPDP_OK;
 }
 
-template <int RB>
-hipError_t launch_shrink_rb(const ShrinkArgs& a, dim3 grid, hipStream_t st) {
-  hipLaunchKernelGGL(shrink_kernel<RB>, grid, dim3(kThreads), kWaves * kTile * 16 * RB * 4, st, a);
-  return hipGetLastError();
-}
-hipError_t launch_shrink(const ShrinkArgs& a, dim3 grid, hipStream_t st) {
-  if (a.rank <= 16) return launch_shrink_rb<1>(a, grid, st);
-  if (a.rank <= 32) return launch_shrink_rb<2>(a, grid, st);
-  if (a.rank <= 64) return launch_shrink_rb<4>(a, grid, st);
-  return launch_shrink_rb<8>(a, grid, st);
-}
-
-template <int RB>
-hipError_t launch_expand_rb(const ExpandArgs& a, dim3 grid, hipStream_t st) {
-  const int lds = ExpandCfg<RB>::kLds;
+template <int RB, int T>
+hipError_t launch_shrink_form(const ShrinkArgs& a, dim3 grid, hipStream_t st) {
+  const int lds = kWaves * T * 16 * RB * 4;
   if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(expand_kernel<RB>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(shrink_kernel<RB, T>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(expand_kernel<RB>, grid, dim3(kThreads), lds, st, a);
+  hipLaunchKernelGGL((shrink_kernel<RB, T>), grid, dim3(kThreads), lds, st, a);
   return hipGetLastError();
 }
-hipError_t launch_expand(ExpandArgs& a, int banks, long long tiles, int cus, hipStream_t st) {
-  int widest = 0;
-  for (int i = 0; i < banks; ++i) widest = std::max(widest, a.m[i].width);
-  const int blocks = (widest + kBlock - 1) / kBlock;
-  // a workgroup keeps its tokens' activations for several blocks where that
-  // leaves eight workgroups per CU
-  a.blocks = (int)std::max<long long>(1, std::min<long long>(8, blocks * tiles * banks / (8ll * cus)));
-  const dim3 grid((unsigned)((blocks + a.blocks - 1) / a.blocks), (unsigned)tiles, (unsigned)banks);
-  if (a.rank <= 16) return launch_expand_rb<1>(a, grid, st);
-  if (a.rank <= 32) return launch_expand_rb<2>(a, grid, st);
-  if (a.rank <= 64) return launch_expand_rb<4>(a, grid, st);
-  return launch_expand_rb<8>(a, grid, st);
+template <int RB>
+hipError_t launch_shrink_rb(const ShrinkArgs& a, int tile, dim3 grid, hipStream_t st) {
+  return tile == 16   ? launch_shrink_form<RB, 16>(a, grid, st)
+         : tile == 32 ? launch_shrink_form<RB, 32>(a, grid, st)
+                      : launch_shrink_form<RB, 64>(a, grid, st);
+}
+hipError_t launch_shrink(const ShrinkArgs& a, int tile, dim3 grid, hipStream_t st) {
+  if (a.rank <= 16) return launch_shrink_rb<1>(a, tile, grid, st);
+  if (a.rank <= 32) return launch_shrink_rb<2>(a, tile, grid, st);
+  if (a.rank <= 64) return launch_shrink_rb<4>(a, tile, grid, st);
+  return launch_shrink_rb<8>(a, tile, grid, st);
 }
 
-hipError_t launch_outer(const OuterArgs& a, int widest, hipStream_t st) {
-  const dim3 grid((unsigned)((widest + kCols - 1) / kCols), (unsigned)a.splits, (unsigned)(2 * a.count));
-  if (a.rank <= 32)
-    hipLaunchKernelGGL(outer_kernel<1>, grid, dim3(kThreads), 0, st, a);
-  else if (a.rank <= 64)
-    hipLaunchKernelGGL(outer_kernel<2>, grid, dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL(outer_kernel<4>, grid, dim3(kThreads), 0, st, a);
+template <int RB, int T, bool FUSED>
+hipError_t launch_expand_form(const ExpandArgs& a, dim3 grid, hipStream_t st) {
+  constexpr int W = FUSED ? kFusedWaves : kWaves;
+  const int lds = ExpandCfg<RB, T, W>::kLds;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(expand_kernel<RB, T, FUSED>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((expand_kernel<RB, T, FUSED>), grid, dim3(64 * W), lds, st, a);
   return hipGetLastError();
+}
+template <int RB>
+hipError_t launch_expand_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_t st) {
+  return tile == 16 ? launch_expand_form<RB, 16, false>(a, grid, st) : launch_expand_form<RB, 32, false>(a, grid, st);
+}
+hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused, int cus, hipStream_t st) {
+  // (64 tokens of a workgroup of expand_kernel took 1.2 to 3.4 times as long)
+  a.subs = p.tile > 32 ? p.tile / 32 : 1;
+  const long long tiles = p.tiles * a.subs;
+  int widest = 0;
+  for (int i = 0; i < banks; ++i) widest = std::max(widest, a.m[i].width);
+  const int block = kCols * (fused ? kFusedWaves : kWaves);
+  const int blocks = (widest + block - 1) / block;
+  // a workgroup keeps its tokens' activations for several blocks where that
+  // leaves the three workgroups that a CU holds (2048 tokens of rank 32, 28672
+  // wide, with 2 / 3 / 5 / 8 blocks: 70 / 67 / 61 / 72 us; 4096 of rank 64, 5120
+  // wide, with 2 / 4 / 8: 37 / 34 / 35)
+  const long long fill = (fused ? 1ll : 3ll) * cus;
+  a.blocks = (int)std::max<long long>(1, std::min<long long>(5, (blocks * tiles * banks + fill - 1) / fill));
+  const dim3 grid((unsigned)((blocks + a.blocks - 1) / a.blocks), (unsigned)tiles, (unsigned)banks);
+  if (fused)
+    return a.rank <= 16   ? launch_expand_form<1, 16, true>(a, grid, st)
+           : a.rank <= 32 ? launch_expand_form<2, 16, true>(a, grid, st)
+                          : launch_expand_form<4, 16, true>(a, grid, st);
+  if (a.rank <= 16) return launch_expand_rb<1>(a, p.tile, grid, st);
+  if (a.rank <= 32) return launch_expand_rb<2>(a, p.tile, grid, st);
+  if (a.rank <= 64) return launch_expand_rb<4>(a, p.tile, grid, st);
+  return launch_expand_rb<8>(a, p.tile, grid, st);
+}
+
+template <int RB>
+hipError_t launch_outer_rb(const OuterArgs& a, int widest, hipStream_t st) {
+  // four workgroups a piece, or up to 64 where there are few pieces
+  const unsigned share = (unsigned)std::max(4, std::min(64, 256 / (a.splits * a.count)));
+  hipLaunchKernelGGL(pack_kernel<RB>, dim3(share, (unsigned)a.splits, (unsigned)(2 * a.count)), dim3(kThreads), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)((widest + kCols - 1) / kCols), (unsigned)a.splits, (unsigned)(2 * a.count));
+  hipLaunchKernelGGL(outer_kernel<RB>, grid, dim3(kThreads), 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_outer(const OuterArgs& a, int widest, hipStream_t st) {
+  if (a.rank <= 32) return launch_outer_rb<1>(a, widest, st);
+  if (a.rank <= 64) return launch_outer_rb<2>(a, widest, st);
+  return launch_outer_rb<4>(a, widest, st);
 }
 
 int check_banks(const spdp_adapters_t* banks, int32_t n_banks, int64_t n_tokens) {
@@ -709,13 +930,28 @@ struct AdaptPlan {
   SortPlan sort;
   Ranges r[kMaxBanks];
   int splits;  // the most of them
+  bool fused;
   size_t bytes;
 };
 void plan_adapt(const spdp_adapters_t* banks, int n_banks, long long n_tokens, bool ids, int cus, AdaptPlan* p) {
-  p->sort = plan_sort(n_tokens, banks[0].count, ids, false);
+  std::memset(p, 0, sizeof(*p));
+  p->sort = plan_sort(n_tokens, banks[0].count, n_banks, ids, false, cus);
   p->bytes = p->sort.bytes;
   p->splits = 1;
+  // The fused form, where a workgroup's own pass over the first factor (at 16,
+  // 32 or 64 ranks) is short and the workgroups that make it are few. Two
+  // launches -> fused, us per pass, called in sequence and from a graph: one
+  // token of rank 8, 1024 wide, 11.4 / 7.0 -> 8.7 / 5.1; 16 requests of rank 16,
+  // three 4096 wide, 12.9 / 9.7 -> 10.7 / 10.5; 32 of them 12.8 / 11.9 -> 16.7 /
+  // 17.1; one of rank 32, three 4096 wide, 13.0 / 9.2 -> 13.0 / 12.9.
+  long long wgs = 0;
+  p->fused = !p->sort.sorted && p->sort.tile == 16 && banks[0].rank <= 64;
   for (int i = 0; i < n_banks; ++i) {
+    p->fused = p->fused && (banks[i].rank + 15) / 16 * 16 * banks[i].cols <= 1 << 16;
+    wgs += p->sort.tiles * ((banks[i].rows + kCols * kFusedWaves - 1) / (kCols * kFusedWaves));
+  }
+  p->fused = p->fused && 2 * wgs <= 3 * cus;
+  for (int i = 0; i < n_banks && !p->fused; ++i) {
     p->r[i] = shrink_ranges(banks[i].cols, p->sort.tiles, n_banks, cus);
     p->splits = std::max(p->splits, p->r[i].splits);
     p->bytes += part_bytes(n_tokens, banks[i].rank, p->r[i].splits);
@@ -726,10 +962,10 @@ struct GradPlan {
   SortPlan sort;
   Ranges r;
   int splits;
-  size_t part, u, outer[2], bytes;
+  size_t part, u, outer[2], packed, down, most, bytes;
 };
 void plan_grad(const spdp_adapters_t* m, long long n_tokens, bool ids, int cus, GradPlan* p) {
-  p->sort = plan_sort(n_tokens, m->count, ids, true);
+  p->sort = plan_sort(n_tokens, m->count, 1, ids, true, cus);
   p->r = shrink_ranges(m->rows, p->sort.tiles, 1, cus);
   p->splits = outer_splits(m, n_tokens, cus);
   p->part = part_bytes(n_tokens, m->rank, p->r.splits);
@@ -737,10 +973,14 @@ void plan_grad(const spdp_adapters_t* m, long long n_tokens, bool ids, int cus, 
   const size_t each = (size_t)p->splits * m->count * m->rank * 4;
   p->outer[0] = p->splits > 1 ? aligned(each * m->cols) : 0;
   p->outer[1] = p->splits > 1 ? aligned(each * m->rows) : 0;
-  p->bytes = p->sort.bytes + p->part + p->u + p->outer[0] + p->outer[1];
+  p->packed = packed_bytes(m, n_tokens, p->splits);
+  p->down = aligned((size_t)m->count * p->splits * 4);
+  p->most = aligned((size_t)n_tokens * 8);
+  p->bytes = p->sort.bytes + p->part + p->u + p->outer[0] + p->outer[1] + 2 * (p->packed + p->down) + p->most;
 }
 
 int check_workspace(const void* workspace, size_t have, size_t need) {
+  if (need == 0) return SPDP_OK;
   if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(SPDP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   if (have < need)
@@ -806,12 +1046,14 @@ int adapt(const spdp_adapters_t* banks, int32_t n_banks, const uint16_t* const* 
   for (int i = 0; i < n_banks; ++i) {
     const spdp_adapters_t& b = banks[i];
     float* const part = reinterpret_cast<float*>(ws);
-    ws += part_bytes(n_tokens, b.rank, p.r[i].splits);
+    if (!p.fused) ws += part_bytes(n_tokens, b.rank, p.r[i].splits);
     sa.m[i] = Shrink{X[i], b.a, part, (int)b.cols, p.r[i].per};
-    ea.m[i] = Expand{part, b.b, b.scale, base[i], Y[i], H ? H[i] : nullptr, (int)b.rows, p.r[i].splits};
+    ea.m[i] = Expand{part, b.b, b.scale, base[i], Y[i], H ? H[i] : nullptr, nullptr, nullptr, X[i], b.a,
+                       (int)b.rows, p.fused ? 1 : p.r[i].splits, (int)b.cols};
   }
-  hipError_t e = launch_shrink(sa, dim3((unsigned)p.sort.tiles, (unsigned)p.splits, (unsigned)n_banks), s);
-  if (e == hipSuccess) e = launch_expand(ea, n_banks, p.sort.tiles, cus, s);
+  hipError_t e = hipSuccess;
+  if (!p.fused) e = launch_shrink(sa, p.sort.tile, dim3((unsigned)p.sort.tiles, (unsigned)p.splits, (unsigned)n_banks), s);
+  if (e == hipSuccess) e = launch_expand(ea, n_banks, p.sort, p.fused, cus, s);
   return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");
 }
 
@@ -867,6 +1109,9 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   float* const u = reinterpret_cast<float*>(ws + p.part);
   float* const pa = reinterpret_cast<float*>(ws + p.part + p.u);
   float* const pb = reinterpret_cast<float*>(ws + p.part + p.u + p.outer[0]);
+  unsigned char* const packed = ws + p.part + p.u + p.outer[0] + p.outer[1];
+  float* const down = reinterpret_cast<float*>(packed + 2 * p.packed);
+  float* const most = reinterpret_cast<float*>(packed + 2 * (p.packed + p.down));
   ShrinkArgs sa;
   ExpandArgs ea;
   OuterArgs oa;
@@ -876,13 +1121,14 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   sa.t = ea.t = t;
   sa.rank = ea.rank = oa.rank = bank->rank;
   sa.m[0] = Shrink{dY, bank->b, part, (int)bank->rows, p.r.per};
-  ea.m[0] = Expand{part, bank->a, bank->scale, base, dX, u, (int)bank->cols, p.r.splits};
-  hipError_t e = launch_shrink(sa, dim3((unsigned)p.sort.tiles, (unsigned)p.r.splits, 1), s);
-  if (e == hipSuccess) e = launch_expand(ea, 1, p.sort.tiles, cus, s);
+  ea.m[0] = Expand{part, bank->a, bank->scale, base, dX, u, most, H, nullptr, nullptr, (int)bank->cols, p.r.splits, 0};
+  hipError_t e = launch_shrink(sa, p.sort.tile, dim3((unsigned)p.sort.tiles, (unsigned)p.r.splits, 1), s);
+  if (e == hipSuccess) e = launch_expand(ea, 1, p.sort, false, cus, s);
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   const bool split = p.splits > 1;
-  oa.m[0] = Outer{u, X, split ? pa : dA, (int)bank->cols};
-  oa.m[1] = Outer{H, dY, split ? pb : dB, (int)bank->rows};
+  oa.m[0] = Outer{u, X, split ? pa : dA, most, packed, down, (int)bank->cols};
+  oa.m[1] = Outer{H, dY, split ? pb : dB, most + n_tokens, packed + p.packed,
+                  down + p.down / 4, (int)bank->rows};
   oa.scale = bank->scale;
   oa.perm = t.perm;
   oa.first = first;

@@ -264,8 +264,8 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   }
 }
 
-// The workgroups' sums, added in a fixed order: each wave every 16th, the
-// waves one after another.
+// The workgroups' sums, added in a fixed order: 16 columns a workgroup, each
+// group of 16 threads every 64th sum, the groups one after another.
 struct SumArgs {
   const float* part[kMaxInputs];
   float* out[kMaxInputs];
@@ -273,17 +273,19 @@ struct SumArgs {
   int dim;
 };
 __global__ __launch_bounds__(1024) void heads_sum_kernel(SumArgs a) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i = (int)blockIdx.x * 64 + lane;
+  __shared__ float red[64][16];
+  const int col = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int i = (int)blockIdx.x * 16 + col;
   const int y = blockIdx.y;
   float sum = 0.0f;
-  if (i < a.dim)
-    for (int q = wave; q < a.n[y]; q += 16) sum += a.part[y][(size_t)q * a.dim + i];
-  red[wave][lane] = sum;
+  if (i < a.dim) {
+#pragma unroll 8
+    for (int q = group; q < a.n[y]; q += 64) sum += a.part[y][(size_t)q * a.dim + i];
+  }
+  red[group][col] = sum;
   __syncthreads();
-  if (wave == 0 && i < a.dim) {
-    for (int w = 1; w < 16; ++w) sum += red[w][lane];
+  if (group == 0 && i < a.dim) {
+    for (int w = 1; w < 64; ++w) sum += red[w][col];
     a.out[y][i] = sum;
   }
 }
@@ -467,7 +469,7 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
     launch<1, 4>(a, back, grid, s);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && sums > 0) {
-    hipLaunchKernelGGL(heads_sum_kernel, dim3((unsigned)((r->dim + 63) / 64), (unsigned)sums), dim3(1024), 0, s, sum);
+    hipLaunchKernelGGL(heads_sum_kernel, dim3((unsigned)((r->dim + 15) / 16), (unsigned)sums), dim3(1024), 0, s, sum);
     e = hipGetLastError();
   }
   return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");

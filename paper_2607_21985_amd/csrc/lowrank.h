@@ -36,7 +36,7 @@ struct Shrink {
   const uint16_t* factor;
   float* part;
   int width;
-  int per;  // steps of 32 columns per split
+  int per;  // steps of 64 columns per split
 };
 struct ShrinkArgs {
   Shrink m[kMaxBanks];
@@ -45,7 +45,9 @@ struct ShrinkArgs {
 };
 
 // out [tokens, width] = base + scale * part's sum times factor
-// [adapter][rank][width]; the sum to `keep` [token][rank] unless NULL
+// [adapter][rank][width]; the sum to `keep` [token][rank] unless NULL; the
+// largest magnitude of each token's sum and of its `other` [token][rank] to
+// `most` [2][token] unless NULL
 struct Expand {
   const float* part;
   const uint16_t* factor;
@@ -53,14 +55,20 @@ struct Expand {
   const uint16_t* base;
   uint16_t* out;
   float* keep;
+  float* most;
+  const float* other;
+  const uint16_t* in;            // the fused form's: part is computed from it
+  const uint16_t* first_factor;  // and from this, as by Shrink
   int width;
   int splits;
+  int in_width;
 };
 struct ExpandArgs {
   Expand m[kMaxBanks];
   Tokens t;
   int rank;
   int blocks;  // 256-column blocks per workgroup
+  int subs;    // parts of a tile, each a workgroup's
 };
 
 // out [adapter][rank][width] = scale * the sum over an adapter's tokens of
@@ -69,6 +77,9 @@ struct Outer {
   const float* act;      // [token][rank]
   const uint16_t* in;    // [token][width]
   float* out;            // [adapter][rank][width], or [split][adapter][rank][width]
+  const float* most;     // [token]: the largest magnitude of act
+  unsigned char* packed; // the activations as operands
+  float* down;           // [adapter][split]: what their scale has to be undone with
   int width;
 };
 struct OuterArgs {

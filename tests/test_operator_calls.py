@@ -87,9 +87,9 @@ expect("tokens", U, adapt(n=(1 << 20) + 1, room=1 << 30))
 expect("null entry", I, adapt(x=[None]))
 expect("null output", I, adapt(y=[None]))
 expect("null h", I, adapt(h=[None]))
-expect("no workspace", I, adapt(ws=None))
-expect("small workspace", I, adapt(room=need([bank()], 40)[1] - 1))
-expect("odd workspace", I, adapt(ws=WS + 128))
+expect("no workspace", I, adapt(n=200, ws=None))
+expect("small workspace", I, adapt(n=200, room=need([bank()], 200)[1] - 1))
+expect("odd workspace", I, adapt(n=200, ws=WS + 128))
 expect("Y in X", I, adapt(y=[X + 40 * 128 * 2 - 2]))
 expect("Y partly in its base", I, adapt(y=[BASE + 512]))
 expect("Y in another's base", I, adapt([bank(), bank()], y=[OUT, BASE]))
@@ -185,12 +185,14 @@ expect("no place", I, L.spdp_spmm_grad_workspace(m._h, 90, None))
 def test_what_the_calls_launch(fake_hip):  # noqa: F811
     out = run(fake_hip, "\n".join([BODY, """
 def names():
-    return [next(k for k in ("sort", "shrink", "expand", "outer_reduce", "outer", "heads_sum", "heads", "grad_plain", "grad", "reduce")
+    return [next(k for k in ("sort", "shrink", "expand", "pack", "outer_reduce", "outer", "heads_sum", "heads", "grad_plain", "grad", "reduce")
                  if k in name) for name, _ in launches()]
 log()
 assert adapt(n=1) == 0
 out["one token"] = names()
-assert adapt(n=64) == 0
+assert adapt([bank(cols=8192, rank=32)], n=1) == 0
+out["a large first factor"] = names()
+assert adapt([bank(count=1)], n=64) == 0
 out["64"] = names()
 assert adapt(n=65) == 0
 out["65"] = names()
@@ -215,10 +217,11 @@ for n in (1, 31, 64, 65, 1000, 5000, 1 << 20):
             for ids in (0, 1):
                 assert need([bank(rank=rank, count=count)], n, ids)[0] == 0
 """]))
-    assert out["one token"] == out["64"] == out["one adapter"] == ["shrink", "expand"]
+    assert out["one token"] == ["expand"]
+    assert out["a large first factor"] == out["64"] == out["one adapter"] == ["shrink", "expand"]
     assert out["65"] == ["sort", "shrink", "expand"]
-    assert out["grad"] == ["sort", "shrink", "expand", "outer"]
-    assert out["grad of many tokens"] == ["shrink", "expand", "outer", "outer_reduce"]
+    assert out["grad"] == ["sort", "shrink", "expand", "pack", "outer"]
+    assert out["grad of many tokens"] == ["shrink", "expand", "pack", "outer", "outer_reduce"]
     assert out["heads"] == out["heads grad without weights"] == ["heads"]
     assert out["heads grad"] == ["heads", "heads_sum"]
     assert out["mallocs"] == 0
