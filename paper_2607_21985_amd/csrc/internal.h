@@ -40,6 +40,7 @@ struct spdp_matrix {
   uint32_t* d_gate = nullptr;  // what a gated call decided (launch.h), behind the offsets
   int chunks = 0;       // chunks (64 columns) of a stripe: those that hold a column below cols
   int chunk_bytes = 0;  // LDS bytes that hold any chunk's values
+  int run_bytes[2] = {0, 0};  // that hold the values of any 2 and any 4 chunks from a multiple of 2 and 4 on
   bool finite = true;   // no infinity or NaN among the values (set with the records)
 
   // Split-K workspace: {fp32 partial sum, phase} pairs

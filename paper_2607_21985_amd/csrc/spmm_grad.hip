@@ -42,7 +42,8 @@ struct GradArgs {
   int tk_log2, n_colblocks;
   int n_stripes;
   int per;             // stripes of a split
-  int chunks, slot;
+  int chunks;
+  int run;             // LDS bytes of a stripe's values
 };
 
 // 32 tokens x 32 columns: register e of lane l holds token 8 (e / 4) + 4 (l / 32)
@@ -135,7 +136,7 @@ struct GradCfg {
   static constexpr int kWaves = CG * TG;
   static constexpr int kTokens = 32 * TB * TG;
   static constexpr int kDyBytes = kTokens * 128;
-  static int lds(int slot) { return CG * slot + 2 * kDyBytes + 256; }
+  static int lds(int run) { return 2 * run + 2 * kDyBytes + 256; }
 };
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
   const bool on = chunk0 + (cg >> 1) < chunk1;  // the last workgroup's chunks may be fewer
   const int chunk = on ? chunk0 + (cg >> 1) : chunk0;
   const uint32_t l0 = lds_addr(lds);
-  const uint32_t val = l0, dyl = l0 + (uint32_t)(CG * a.slot), lut = dyl + 2 * C::kDyBytes;
+  const uint32_t val = l0, dyl = l0 + 2u * (uint32_t)a.run, lut = dyl + 2 * C::kDyBytes;
   if (threadIdx.x < 16) {
     const u32x2 s = selectors(threadIdx.x);
     *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(lut + 8 * threadIdx.x) = s;
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
   auto issue_values = [&](int r, int q, const Run& u) __attribute__((always_inline)) {
     if (r >= r1 || u.t1 <= u.t0) return;
     const uint32_t last = u.t1 - u.t0 - 16u;
-    const uint32_t to = val + (uint32_t)(r & 1) * (uint32_t)(CG / 2) * (uint32_t)a.slot;
+    const uint32_t to = val + (uint32_t)(r & 1) * (uint32_t)a.run;
     for (uint32_t at = 1024u * (uint32_t)(W * q + wave); at <= last; at += 3072u * W)
       dma16(a.values, u.t0 + min(at + 16u * (uint32_t)lane, last),
             (uint32_t)__builtin_amdgcn_readfirstlane((int)(to + at)));
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
   auto walk = [&](const Rec& m, int r, const Run& u) __attribute__((always_inline)) {
     Walk k;
     k.mask = half ? m.hi : m.lo;
-    k.p = val + (uint32_t)(r & 1) * (uint32_t)(CG / 2) * (uint32_t)a.slot + (u.tm - u.t0) +
+    k.p = val + (uint32_t)(r & 1) * (uint32_t)a.run + (u.tm - u.t0) +
           ((lane & 1) ? m.offs >> 16 : m.offs & 0xFFFFu) +
           (half ? 2u * (uint32_t)__builtin_popcount(m.lo) : 0u);
     return k;
@@ -375,7 +376,7 @@ constexpr int kLdsMax = 160 * 1024;
 struct Form {
   int tb, cg, tg;
   int tokens() const { return 32 * tb * tg; }
-  int lds(int slot) const { return cg * slot + 2 * tokens() * 128 + 256; }
+  int lds(const spdp_matrix* h) const { return 2 * h->run_bytes[cg / 8] + 2 * tokens() * 128 + 256; }
 };
 constexpr Form kForms[] = {{1, 4, 1}, {2, 4, 1}, {4, 4, 1}, {4, 4, 2}, {1, 8, 1}, {2, 8, 1}, {4, 8, 1}, {8, 8, 1}};
 constexpr int kNumForms = sizeof(kForms) / sizeof(kForms[0]);
@@ -399,7 +400,7 @@ void plan_grad(const spdp_matrix* h, long long n_tokens, GradPlan* p) {
   for (int i = 0; i < kNumForms; ++i) {
     if (forced_form > -2 && forced_form != i) continue;
     const Form& f = kForms[i];
-    if (h->d_rec == nullptr || f.lds(h->chunk_bytes) > kLdsMax ||
+    if (h->d_rec == nullptr || f.lds(h) > kLdsMax ||
         std::min<long long>(n_tokens, f.tokens()) * h->rows * 2 > 1ll << 32 || (n_tokens + f.tokens() - 1) / f.tokens() > 65535)
       continue;
     if (p->form < 0 || f.tokens() <= n_tokens) p->form = i;
@@ -419,7 +420,7 @@ size_t part_bytes(const spdp_matrix* h, long long n_tokens, const GradPlan& p) {
 
 template <int TB, int CG, int TG, bool DYV>
 hipError_t launch_form(const GradArgs& a, dim3 grid, hipStream_t st) {
-  const int lds = GradCfg<TB, CG, TG>::lds(a.slot);
+  const int lds = GradCfg<TB, CG, TG>::lds(a.run);
   const auto kernel = grad_kernel<TB, CG, TG, DYV>;
   if (lds > 64 * 1024) {
     const hipError_t e =
@@ -493,7 +494,7 @@ int spmm_grad(spdp_handle_t h, const uint16_t* dY, int64_t n_tokens, uint16_t* d
   a.n_stripes = (int)h->n_stripes;
   a.per = p.per;
   a.chunks = h->chunks;
-  a.slot = h->chunk_bytes;
+  a.run = p.form >= 0 ? h->run_bytes[kForms[p.form].cg / 8] : 0;
   auto s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)p.blocks, (unsigned)p.tiles, (unsigned)p.splits);
   if (p.form >= 0) {

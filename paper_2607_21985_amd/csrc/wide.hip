@@ -646,6 +646,14 @@ int lay_out_records(spdp_matrix* m) {
   m->d_gate = flag;
   m->chunks = (int)chunks;
   m->chunk_bytes = std::max(1024, (int)((widest + 1023) / 1024 * 1024));
+  for (int i = 0; i < 2; ++i) {
+    const int64_t n = 2 << i;
+    uint32_t run = 0;
+    for (int64_t r = 0; r < m->n_stripes; ++r)
+      for (int64_t c = 0; c < chunks; c += n)
+        run = std::max(run, off[(size_t)(r * chunks + std::min(c + n, chunks))] - off[(size_t)(r * chunks + c)]);
+    m->run_bytes[i] = std::max(1024, (int)((run + 1023) / 1024 * 1024));
+  }
   return SPDP_OK;
 }
 
