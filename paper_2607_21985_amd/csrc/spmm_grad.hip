@@ -114,22 +114,22 @@ __global__ __launch_bounds__(kThreads) void grad_plain_kernel(GradArgs a) {
 // ---------------------------------------------------------------------------
 // The form for handles with word records. CG TG waves own 32 CG columns (CG / 2
 // chunks) and 32 TB TG tokens, each wave 32 columns and 32 TB tokens; lane l has
-// column l mod 32 and, of each 64-row word, the rows 32 (l / 32) .. + 31. Per
-// four rows a lane reads the next four values of its column from LDS (as many
-// are used as the four bits of the bitmap word have ones) and puts them into
-// their places with two byte permutations, whose selectors a table of 16 entries
-// holds. Eight rows are an operand of v_mfma_f32_32x32x16_f16; the tokens'
-// operands come from LDS in the same order of rows. The values are read as two
-// aligned 8-byte words and shifted in registers: a wave's 64 reads of 8 bytes
-// take 6 cycles where all are aligned, 65 where they are not.
+// column l mod 32 and, of each stripe, the rows 128 (l / 32) .. + 127, whose
+// values it walks down. Per four rows it puts the next values (as many as the
+// four bits of the bitmap have ones) into their places with two byte
+// permutations, whose selectors a table of 16 entries holds. Eight rows are an
+// operand of v_mfma_f32_32x32x16_f16; the tokens' operands come from LDS in the
+// same order of rows. The values are read as aligned 8-byte words, of which the
+// last one is kept, and shifted in registers: a wave's 64 reads of 8 bytes take
+// 6 cycles where all are aligned, 65 where they are not.
 //
-// A step is 8 rows of both halves of the lanes; a word has four. During the
-// MFMAs of a step the next one's operands are built and read, across words, too.
-// Values (per stripe one contiguous run) arrive by DMA in three parts during the
-// stripe before, the tokens' 64 rows of dY one word ahead, 16-byte piece p of
-// token t at place p ^ (t / 2 mod 8). The one barrier per word stands before
-// its last step, when all of the word's operands have been read: what is
-// requested behind it may overwrite them.
+// A step is 8 rows of both halves of the lanes; a quarter of a stripe has four.
+// During the MFMAs of a step the next one's operands are built and read, across
+// quarters, too. Values (per stripe one contiguous run) arrive by DMA in three
+// parts during the stripe before, a quarter's 64 rows of dY one quarter ahead,
+// 16-byte piece p of token t at place p ^ (t / 2 mod 8). The one barrier per
+// quarter stands in its last step, when all of the quarter's operands have been
+// read: what is requested behind it may overwrite them.
 
 template <int TB, int CG, int TG>
 struct GradCfg {
@@ -141,22 +141,32 @@ struct GradCfg {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// Four rows of a column: the 16 bytes of LDS that hold its next four values,
-// and the selectors for the rows' bits.
+// Where a lane is in its column: the aligned 8 bytes of LDS that hold its next
+// value, and the 8 behind them.
+struct Window {
+  u32x2 a, b;
+  uint32_t at;
+};
+// Four rows of a column, requested: the 8 bytes behind those that hold the first
+// value, and the selectors for the rows' bits.
 struct Quad {
-  u32x2 a, b, sel;
+  u32x2 behind, sel;
   uint32_t p;
   __device__ __forceinline__ void read(uint32_t at, uint32_t selectors_at) {
     typedef const __attribute__((address_space(3))) u32x2* lds8;
     p = at;
-    a = *(lds8)(uintptr_t)(at & ~7u);
-    b = *(lds8)(uintptr_t)((at & ~7u) + 8u);
+    behind = *(lds8)(uintptr_t)((at & ~7u) + 8u);
     sel = *(lds8)(uintptr_t)selectors_at;
   }
-  // the rows' fp16, 0 where the bit is clear
-  __device__ __forceinline__ u32x2 rows() const {
+  // the rows' fp16, 0 where the bit is clear; moves the window on (four rows
+  // have at most 8 bytes of values, so by one word at most)
+  __device__ __forceinline__ u32x2 rows(Window& w) const {
+    const bool next = (p & ~7u) != w.at;
+    w.a = next ? w.b : w.a;
+    w.b = behind;
+    w.at = p & ~7u;
     const bool up = p & 4u;
-    const uint32_t x0 = up ? a[1] : a[0], x1 = up ? b[0] : a[1], x2 = up ? b[1] : b[0];
+    const uint32_t x0 = up ? w.a[1] : w.a[0], x1 = up ? w.b[0] : w.a[1], x2 = up ? w.b[1] : w.b[0];
     const uint32_t lo = __builtin_amdgcn_alignbyte(x1, x0, p), hi = __builtin_amdgcn_alignbyte(x2, x1, p);
     return u32x2{__builtin_amdgcn_perm(hi, lo, sel[0]), __builtin_amdgcn_perm(hi, lo, sel[1])};
   }
@@ -174,12 +184,6 @@ __device__ __forceinline__ u32x2 selectors(uint32_t b) {
   }
   return s;
 }
-
-// Where a lane is in its column: the bits of the word's rows that it has, and
-// the LDS address of the next value.
-struct Walk {
-  uint32_t mask, p;
-};
 
 // DYV: dY rows are 16-byte aligned (else they are read at any address)
 template <int TB, int CG, int TG, bool DYV>
@@ -226,10 +230,11 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
             (uint32_t)__builtin_amdgcn_readfirstlane((int)(to + at)));
   };
   const int piece = (lane & 7) ^ (4 * (wave & 1) + (lane >> 4));
-  // the 64 rows of word `word` (from the matrix's first) of dY into buffer b: 8
+  // the 64 rows of quarter `word` (from the matrix's first) of dY into buffer b: 8
   // tokens a wave and round
   auto issue_dy = [&](int word, int b) __attribute__((always_inline)) {
     if (word >= 4 * r1) return;
+    const int m0 = kTM * (word >> 2) + 32 * (word & 3);
 #pragma unroll
     for (int i = 0; i < (4 * TB * TG + W - 1) / W; ++i) {
       const int t8 = W * i + wave;
@@ -238,9 +243,9 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
       int lane8 = lane >> 3;
       asm volatile("" : "+v"(lane8));  // (keeps the tokens' offsets out of registers between words)
       const uint32_t t = (uint32_t)min(8 * t8 + lane8, last_tok);
-      const int m = 64 * word + 8 * piece;
+      const int m = m0 + 128 * (piece >> 2) + 8 * (piece & 3);
       if constexpr (DYV) {
-        if (64 * word + 64 <= a.rows || m < a.rows)
+        if (m0 + 160 <= a.rows || m < a.rows)
           dma16(dyb, (t * (uint32_t)a.rows + (uint32_t)m) * 2u, (uint32_t)__builtin_amdgcn_readfirstlane((int)to));
         else
           *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + 16u * (uint32_t)lane) = u32x4{0, 0, 0, 0};
@@ -251,106 +256,116 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
       }
     }
   };
-  // the lane's record of a word: its column's bits and, for a pair of columns,
-  // the byte offsets of the word's first value in the chunk
+  // of a stripe's records: the bits of the lane's 128 rows, and, for a pair of
+  // columns, the byte offsets in the chunk of the first value
   struct Rec {
-    uint32_t lo, hi, offs;
+    uint2 w0, w1;
+    uint32_t offs;
   };
-  const unsigned char* const rec_at =
-      a.rec + (size_t)chunk * kChunkRecBytes + (4 * (2 * (cg & 1) + (lane >> 4 & 1))) * kRecBytes;
   const int c16 = lane & 15;
-  auto load_rec1 = [&](int word, Rec& m) __attribute__((always_inline)) {
-    word = min(word, 4 * r1 - 1);
-    const unsigned char* p = rec_at + (size_t)(word >> 2) * a.chunks * kChunkRecBytes + (word & 3) * kRecBytes;
-    const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * c16);
-    m.lo = w.x;
-    m.hi = w.y;
+  const unsigned char* const rec_at =
+      a.rec + (size_t)chunk * kChunkRecBytes + (4 * (2 * (cg & 1) + (lane >> 4 & 1)) + 2 * half) * kRecBytes;
+  auto load_rec1 = [&](int r, Rec& m) __attribute__((always_inline)) {
+    const unsigned char* p = rec_at + (size_t)min(r, r1 - 1) * a.chunks * kChunkRecBytes;
+    m.w0 = *reinterpret_cast<const uint2*>(p + 8 * c16);
+    m.w1 = *reinterpret_cast<const uint2*>(p + kRecBytes + 8 * c16);
     m.offs = *reinterpret_cast<const uint32_t*>(p + 128 + 4 * (c16 >> 1));
   };
+  // and from them the bits and the LDS address of the first value
+  struct Walk {
+    uint32_t mask[4], p;
+  };
   auto walk = [&](const Rec& m, int r, const Run& u) __attribute__((always_inline)) {
-    Walk k;
-    k.mask = half ? m.hi : m.lo;
-    k.p = val + (uint32_t)(r & 1) * (uint32_t)a.run + (u.tm - u.t0) +
-          ((lane & 1) ? m.offs >> 16 : m.offs & 0xFFFFu) +
-          (half ? 2u * (uint32_t)__builtin_popcount(m.lo) : 0u);
-    return k;
+    return Walk{{m.w0.x, m.w0.y, m.w1.x, m.w1.y},
+                val + (uint32_t)(r & 1) * (uint32_t)a.run + (u.tm - u.t0) + ((lane & 1) ? m.offs >> 16 : m.offs & 0xFFFFu)};
   };
 
   float16v acc[TB];
 #pragma unroll
   for (int j = 0; j < TB; ++j) acc[j] = float16v{};
   Run here = run_of(r0), next = run_of(r0 + 1);
-  Rec rec, rec1, rec2;
+  Rec rec;
 #pragma unroll
   for (int q = 0; q < 3; ++q) issue_values(r0, q, here);
   issue_dy(4 * r0, 0);
   issue_dy(4 * r0 + 1, 1);
-  load_rec1(4 * r0, rec1);
-  load_rec1(4 * r0 + 1, rec2);
-  load_rec1(4 * r0 + 2, rec);
+  load_rec1(r0, rec);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  Walk k = walk(rec, r0, here);
   issue_values(r0 + 1, 0, next);
-  Walk k0 = walk(rec1, r0, here), k1 = walk(rec2, r0, here);
 
   half8 x[2][TB];
   Quad q[2];
+  Window win;
+  u32x2 first;  // the window's first word at the start of a stripe
   const uint32_t db = dyl + (uint32_t)(4096 * TB * tg) + 128u * (uint32_t)(lane & 31);
   auto read_x = [&](int v, int j, int t) __attribute__((always_inline)) {
     const uint32_t place = 16u * (uint32_t)((4 * half + j) ^ (lane >> 1 & 7));
     return *(const __attribute__((address_space(3))) half8*)(uintptr_t)(db + (uint32_t)((v & 1) * C::kDyBytes) + 4096u * t + place);
   };
-  auto read_q = [&](Walk& k, int j) __attribute__((always_inline)) {
+  // step s of 16 of a stripe
+  auto read_q = [&](Walk& w, int s) __attribute__((always_inline)) {
+    if (s == 0) first = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)(w.p & ~7u);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint32_t b = k.mask >> (8 * j + 4 * i) & 15u;
-      q[i].read(k.p, lut + 8u * b);
-      k.p += 2u * (uint32_t)__builtin_popcount(b);
+      const uint32_t b = w.mask[s >> 2] >> (8 * (s & 3) + 4 * i) & 15u;
+      q[i].read(w.p, lut + 8u * b);
+      w.p += 2u * (uint32_t)__builtin_popcount(b);
     }
   };
   u32x2 w[2];
-  read_q(k0, 0);
+  auto build = [&](int s, int i) __attribute__((always_inline)) {
+    if (s == 0 && i == 0) {
+      win.a = first;
+      win.at = q[0].p & ~7u;
+    }
+    w[i] = q[i].rows(win);
+  };
+  read_q(k, 0);
+  build(0, 0);
+  build(0, 1);
+  read_q(k, 1);
+  // the tokens' operands are read kLead MFMAs ahead
+  constexpr int kLead = TB < 4 ? TB : 4;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) w[i] = q[i].rows();
-  read_q(k0, 1);
-#pragma unroll
-  for (int t = 0; t < TB; ++t) x[0][t] = read_x(0, 0, t);
+  for (int t = 0; t < kLead; ++t) x[0][t] = read_x(0, 0, t);
 
   for (int r = r0; r < r1; ++r) {
     Run after;
+    Walk kn;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      Walk k2;
+    for (int s = 0; s < 16; ++s) {
+      const int v = s >> 2, j = s & 3;
+      if (s == 8) after = run_of(r + 2);
+      const half8 now = __builtin_bit_cast(half8, u32x4{w[0][0], w[0][1], w[1][0], w[1][1]});
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (j == 3) {
+      for (int t = 0; t < TB; ++t) {
+        if (j == 3 && t == TB - kLead) {
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          // the record is there: taken now, for the compiler's own wait for it
-          // would count the loads requested below
-          asm volatile("" : "+v"(rec.lo), "+v"(rec.hi), "+v"(rec.offs));
-          k2 = walk(rec, v < 2 ? r : r + 1, v < 2 ? here : next);
-          load_rec1(4 * r + v + 3, rec);
+          if (v == 2) {
+            // the record is there: taken now, for the compiler's own wait for it
+            // would count the loads requested below
+            asm volatile("" : "+v"(rec.w0.x), "+v"(rec.w0.y), "+v"(rec.w1.x), "+v"(rec.w1.y), "+v"(rec.offs));
+            kn = walk(rec, r + 1, next);
+          }
+          if (v == 1) load_rec1(r + 1, rec);
           issue_dy(4 * r + v + 2, v & 1);
           if (v == 3)
             issue_values(r + 2, 0, after);
           else if (v < 2)
             issue_values(r + 1, v + 1, next);
         }
-        if (v == 2 && j == 0) after = run_of(r + 2);
-        const half8 now = __builtin_bit_cast(half8, u32x4{w[0][0], w[0][1], w[1][0], w[1][1]});
+        const int ahead = s * TB + t + kLead;
+        x[ahead / TB & 1][ahead % TB] = read_x(ahead / TB >> 2, ahead / TB & 3, ahead % TB);
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[j & 1][t], now, acc[t], 0, 0, 0);
+        if (t == 0) build((s + 1) & 15, 0);
+        if (t == (TB > 1 ? 1 : 0)) build((s + 1) & 15, 1);
+        if (t == (TB > 2 ? 2 : TB - 1)) read_q(s < 14 ? k : kn, (s + 2) & 15);
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int t = 0; t < TB; ++t) {
-          x[(j + 1) & 1][t] = read_x(j < 3 ? v : v + 1, (j + 1) & 3, t);
-          acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[j & 1][t], now, acc[t], 0, 0, 0);
-          if (t == 0) w[0] = q[0].rows();
-          if (t == (TB > 1 ? 1 : 0)) w[1] = q[1].rows();
-          if (t == (TB > 2 ? 2 : TB - 1)) read_q(j < 2 ? k0 : k1, (j + 2) & 3);
-          __builtin_amdgcn_sched_barrier(0);
-        }
       }
-      k0 = k1;
-      k1 = k2;
     }
+    k = kn;
     here = next;
     next = after;
   }
