@@ -387,13 +387,19 @@ int hip_fail(hipError_t e, const char* what) {
 constexpr int kLdsMax = 160 * 1024;
 
 // The forms: blocks of 32 tokens of a wave, groups of 32 columns and groups of
-// tokens of a workgroup.
+// tokens of a workgroup; and what a quarter of a stripe (64 rows) takes, us, with
+// one, two, ... workgroups on a CU (0: LDS or registers hold no more).
 struct Form {
   int tb, cg, tg;
+  float us[4];
   int tokens() const { return 32 * tb * tg; }
   int lds(const spdp_matrix* h) const { return 2 * h->run_bytes[cg / 8] + 2 * tokens() * 128 + 256; }
 };
-constexpr Form kForms[] = {{1, 4, 1}, {2, 4, 1}, {4, 4, 1}, {4, 4, 2}, {1, 8, 1}, {2, 8, 1}, {4, 8, 1}, {8, 8, 1}};
+constexpr Form kForms[] = {
+    {1, 4, 1, {0.66f, 0.80f, 1.23f, 1.37f}}, {2, 4, 1, {0.76f, 0.90f, 1.11f, 0.0f}},
+    {4, 4, 1, {0.95f, 1.18f, 0.0f, 0.0f}},   {4, 4, 2, {1.25f, 0.0f, 0.0f, 0.0f}},
+    {1, 8, 1, {0.80f, 1.10f, 0.0f, 0.0f}},   {2, 8, 1, {0.89f, 1.20f, 0.0f, 0.0f}},
+    {4, 8, 1, {1.11f, 0.0f, 0.0f, 0.0f}},    {8, 8, 1, {1.74f, 0.0f, 0.0f, 0.0f}}};
 constexpr int kNumForms = sizeof(kForms) / sizeof(kForms[0]);
 
 struct GradPlan {
@@ -407,24 +413,53 @@ int env_int(const char* name, int otherwise) {
   return env ? std::atoi(env) : otherwise;
 }
 
+// us of a form with `splits` ranges of the stripes, by the model that the table
+// above is fitted to (1145 launches of 7 matrices at 16 to 2048 tokens, 7 % rms):
+// rounds of workgroups, 0.7 us each; 3 us and 8 bytes per sum at 5.6 TB/s for the
+// second launch that adds the ranges.
+float model_us(const spdp_matrix* h, const Form& f, long long wgs, int per, int splits, long long n_tokens, int cus) {
+  int most = 1;
+  while (most < 4 && f.us[most] > 0.0f && (most + 1) * f.lds(h) <= kLdsMax) ++most;
+  const long long full = wgs / ((long long)cus * most), rest = wgs - full * cus * most;
+  const int k = (int)((rest + cus - 1) / cus);  // workgroups on a CU in the last round
+  float us = (float)full * (4.0f * (float)per * f.us[most - 1] + 0.7f);
+  if (k > 0) us += 4.0f * (float)per * f.us[k - 1] + 0.7f;
+  if (splits > 1) us += 1.4f + (float)splits * (float)n_tokens * (float)h->cols * 8.0f / 5.6e6f;
+  return us;
+}
+
+// The form and split of the least modelled time, within 256 MB of partial sums.
+// SPDP_GRAD_FORM (a testing aid) forces a form by its place in the table, or the
+// plain one (-1), SPDP_GRAD_SPLITS the ranges.
 void plan_grad(const spdp_matrix* h, long long n_tokens, GradPlan* p) {
   const int cus = std::max(1, h->cus);
   const int forced_splits = env_int("SPDP_GRAD_SPLITS", 0), forced_form = env_int("SPDP_GRAD_FORM", -2);
   const long long stripes = h->n_stripes;
   p->form = -1;
+  p->tiles = (n_tokens + 127) / 128;
+  p->blocks = (int)((h->cols + 63) / 64);
+  float least = 0.0f;
   for (int i = 0; i < kNumForms; ++i) {
-    if (forced_form > -2 && forced_form != i) continue;
     const Form& f = kForms[i];
-    if (h->d_rec == nullptr || f.lds(h) > kLdsMax ||
+    if ((forced_form > -2 && forced_form != i) || h->d_rec == nullptr || f.lds(h) > kLdsMax ||
         std::min<long long>(n_tokens, f.tokens()) * h->rows * 2 > 1ll << 32 || (n_tokens + f.tokens() - 1) / f.tokens() > 65535)
       continue;
-    if (p->form < 0 || f.tokens() <= n_tokens) p->form = i;
+    const long long tiles = (n_tokens + f.tokens() - 1) / f.tokens();
+    const int blocks = (int)((h->cols + 32 * f.cg - 1) / (32 * f.cg));
+    for (int want = forced_splits > 0 ? (int)std::min<long long>(forced_splits, stripes) : 1;; ++want) {
+      const int per = (int)((stripes + want - 1) / want), splits = (int)((stripes + per - 1) / per);
+      const float us = model_us(h, f, tiles * blocks * splits, per, splits, n_tokens, cus);
+      if (p->form < 0 || us < least) {
+        least = us;
+        *p = GradPlan{i, tiles, blocks, per, splits};
+      }
+      if (forced_splits > 0 || want >= 16 || want >= stripes || (float)(want + 1) * n_tokens * h->cols * 4.0f > 256e6f) break;
+    }
   }
-  const int tokens = p->form >= 0 ? kForms[p->form].tokens() : 128, columns = p->form >= 0 ? 32 * kForms[p->form].cg : 64;
-  p->tiles = (n_tokens + tokens - 1) / tokens;
-  p->blocks = (int)((h->cols + columns - 1) / columns);
+  if (p->form >= 0) return;
   const long long wgs = p->tiles * p->blocks;
-  const long long want = std::min<long long>(stripes, forced_splits > 0 ? forced_splits : std::max<long long>(1, std::min<long long>(16, cus / wgs)));
+  const long long want =
+      std::min<long long>(stripes, forced_splits > 0 ? forced_splits : std::max<long long>(1, std::min<long long>(16, cus / wgs)));
   p->per = (int)((stripes + want - 1) / want);
   p->splits = (int)((stripes + p->per - 1) / p->per);
 }
