@@ -35,6 +35,7 @@ struct HeadsInput {
   float* part;         // backward with weights: [workgroup of this input][dim]
   int heads;
   int wg0;             // the input's first workgroup
+  int per;             // heads of a group of lanes, one after another
 };
 struct HeadsArgs {
   HeadsInput m[kMaxInputs];
@@ -46,18 +47,20 @@ struct HeadsArgs {
   int n_tokens;
   int positions;
   int dim, half;
-  int interleaved;
   int lanes;  // of a head: a power of two
-  int per;    // heads of a group of lanes, one after another
 };
 
+// V fp16 as they are in memory
 template <int V>
-__device__ __forceinline__ void load_v(const uint16_t* p, float (&v)[V]) {
+struct Raw {
   uint16_t h[V];
-  __builtin_memcpy(h, p, 2 * V);
+  __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(h, p, 2 * V); }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = __half2float(__ushort_as_half(h[e]));
-}
+    for (int e = 0; e < V; ++e) h[e] = 0;
+  }
+  __device__ __forceinline__ float operator[](int e) const { return __half2float(__ushort_as_half(h[e])); }
+};
 template <int V>
 __device__ __forceinline__ void store_v(uint16_t* p, const float (&v)[V]) {
   uint16_t h[V];
@@ -66,92 +69,62 @@ __device__ __forceinline__ void store_v(uint16_t* p, const float (&v)[V]) {
   __builtin_memcpy(p, h, 2 * V);
 }
 
-// A lane's place in a head: the vectors at a and b (b past the end: none), and
-// how they rotate.
+// A lane's place in a head: the vectors at a and b (past the end: none), and
+// whether they rotate. PAIRS: pairs are neighbours, within a and within b; else
+// a rotates with b.
 struct Slot {
   int a, b;
-  int kind;  // 0: not at all, 1: a with b, 2: neighbours within a and within b
+  bool turns;
 };
-template <int V>
-__device__ __forceinline__ Slot slot_of(int s, int dim, int half, int interleaved) {
-  Slot t;
-  if (!interleaved && s < half / V) {
-    t.a = s * V;
-    t.b = half + s * V;
-    t.kind = 1;
-  } else {
-    const int from = interleaved ? 0 : half / V;
-    t.a = (interleaved ? 0 : 2 * half) + 2 * V * (s - from);
-    t.b = t.a + V;
-    t.kind = interleaved ? 2 : 0;
-  }
-  return t;
+template <int V, bool PAIRS>
+__device__ __forceinline__ Slot slot_of(int s, int half) {
+  if (!PAIRS && s < half / V) return Slot{s * V, half + s * V, true};
+  const int from = PAIRS ? 0 : half / V;
+  const int at = (PAIRS ? 0 : 2 * half) + 2 * V * (s - from);
+  return Slot{at, at + V, PAIRS};
 }
 
-// The rotation of a slot's vectors by the angle's cosine and (sign times) sine.
-template <int V>
+// The rotation of a slot's vectors by the angle's cosine and (sign times) sine;
+// numbers past the leading ones turn by none.
+template <int V, bool PAIRS>
 struct Turn {
-  float c[2][V], s[2][V];
+  static constexpr int kAngles = V;  // PAIRS: V / 2 of a, V / 2 of b
+  float c[kAngles], s[kAngles];
+  __device__ __forceinline__ void load(const HeadsArgs& a, const Slot& t, long long pos, float sign) {
+    const float* const tc = a.cosine + pos * a.half;
+    const float* const ts = a.sine + pos * a.half;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int at = PAIRS ? t.a / 2 + e : t.a + e;  // (b's angles follow a's)
+      const bool in = t.turns && at < a.half;
+      c[e] = in ? tc[at] : 1.0f;
+      s[e] = in ? sign * ts[at] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void apply(float (&x)[2][V]) const {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float& first = PAIRS ? x[2 * e / V][2 * e % V] : x[0][e];
+      float& second = PAIRS ? x[2 * e / V][2 * e % V + (V > 1)] : x[1][e];
+      const float p = first, q = second;
+      first = p * c[e] - q * s[e];
+      second = q * c[e] + p * s[e];
+    }
+  }
 };
-template <int V>
-__device__ __forceinline__ void load_turn(const HeadsArgs& a, const Slot& t, long long pos, float sign, Turn<V>& u) {
-  const float* const c = a.cosine + pos * a.half;
-  const float* const s = a.sine + pos * a.half;
-  if (t.kind == 1) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      u.c[0][e] = c[t.a + e];
-      u.s[0][e] = sign * s[t.a + e];
-    }
-  } else if (t.kind == 2) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int at = k == 0 ? t.a : t.b;
-#pragma unroll
-      for (int e = 0; e < V; e += 2) {
-        const bool in = at + e < 2 * a.half;
-        u.c[k][e] = in ? c[(at + e) / 2] : 1.0f;
-        u.s[k][e] = in ? sign * s[(at + e) / 2] : 0.0f;
-      }
-    }
-  }
-}
-template <int V>
-__device__ __forceinline__ void turn(const Slot& t, const Turn<V>& u, int lead, float (&x)[2][V]) {
-  if (t.kind == 1) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float p = x[0][e], q = x[1][e];
-      x[0][e] = p * u.c[0][e] - q * u.s[0][e];
-      x[1][e] = q * u.c[0][e] + p * u.s[0][e];
-    }
-  } else if (t.kind == 2) {
-    if constexpr (V > 1) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int e = 0; e < V; e += 2)
-          if ((k == 0 ? t.a : t.b) + e < lead) {
-            const float p = x[k][e], q = x[k][e + 1];
-            x[k][e] = p * u.c[k][e] - q * u.s[k][e];
-            x[k][e + 1] = q * u.c[k][e] + p * u.s[k][e];
-          }
-    }
-  }
-}
 
 // A workgroup of an input: its groups of lanes take `per` heads of a token
 // each, the groups of a wave all of one token.
-template <int V, int R, bool BACK>
+template <int V, int R, bool PAIRS, bool BACK>
 __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   int which = 0;
   while (which + 1 < a.inputs && (int)blockIdx.x >= a.m[which + 1].wg0) ++which;
-  const HeadsInput m = a.m[which];
+  const HeadsInput& m = a.m[which];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int groups = 64 / a.lanes;
   const int group = lane / a.lanes, sub = lane % a.lanes;
-  const int chunk = groups * a.per;  // heads of a wave's round
+  const int chunk = groups * m.per;  // heads of a wave's round
   const int chunks = (m.heads + chunk - 1) / chunk;
   const bool norm = m.w != nullptr;
   const float inv_dim = 1.0f / (float)a.dim;
@@ -161,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   float dw[R][2][V];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    t[r] = slot_of<V>(sub + 64 * r, a.dim, a.half, a.interleaved);
+    t[r] = slot_of<V, PAIRS>(sub + 64 * r, a.half);
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -179,28 +152,46 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
     const int pos = a.pos[tok];
     const bool inside = (unsigned)pos < (unsigned)a.positions;
     if (!BACK && !inside) continue;  // a padding token
-    Turn<V> u[R];
+    Turn<V, PAIRS> u[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) load_turn<V>(a, t[r], inside ? pos : 0, BACK ? -1.0f : 1.0f, u[r]);
-    for (int i = 0; i < a.per; ++i) {
+    for (int r = 0; r < R; ++r) u[r].load(a, t[r], inside ? pos : 0, BACK ? -1.0f : 1.0f);
+    // a head's numbers, requested a head ahead
+    Raw<V> nx[R][2], ng[R][2];
+    auto request = [&](int h) __attribute__((always_inline)) {
+      const size_t at = ((size_t)tok * m.heads + h) * a.dim;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int from = k == 0 ? t[r].a : t[r].b;
+          nx[r][k].clear();
+          if (BACK) ng[r][k].clear();
+          if (h < m.heads && inside && from < a.dim) {
+            if (!BACK || norm) nx[r][k].load(m.x + at + from);
+            if (BACK) ng[r][k].load(m.dy + at + from);
+          }
+        }
+    };
+    request(h0 + group);
+    for (int i = 0; i < m.per; ++i) {
       const int h = h0 + i * groups + group;
       const bool on = h < m.heads;
       const size_t at = ((size_t)tok * m.heads + (on ? h : 0)) * a.dim;
       float x[R][2][V], g[R][2][V];
       float sum = 0.0f, dot = 0.0f;
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int e = 0; e < V; ++e) x[r][k][e] = g[r][k][e] = 0.0f;
-          const int from = k == 0 ? t[r].a : t[r].b;
-          if (on && inside && from < a.dim) {
-            if (!BACK || norm) load_v<V>(m.x + at + from, x[r][k]);
-            if (BACK) load_v<V>(m.dy + at + from, g[r][k]);
+          for (int e = 0; e < V; ++e) {
+            x[r][k][e] = nx[r][k][e];
+            g[r][k][e] = BACK ? ng[r][k][e] : 0.0f;
           }
-        }
-        if (BACK) turn<V>(t[r], u[r], 2 * a.half, g[r]);
+      if (i + 1 < m.per) request(h + groups);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (BACK) u[r].apply(g[r]);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -235,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
               o[k][e] = g[r][k][e];
             }
           }
-        if (!BACK) turn<V>(t[r], u[r], 2 * a.half, o);
+        if (!BACK) u[r].apply(o);
         if (on) {
           if (t[r].a < a.dim) store_v<V>(m.y + at + t[r].a, o[0]);
           if (t[r].b < a.dim) store_v<V>(m.y + at + t[r].b, o[1]);
@@ -303,7 +294,7 @@ int hip_fail(hipError_t e, const char* what) {
 // four workgroups per CU result.
 struct HeadsPlan {
   int v, slots, lanes, rounds;  // rounds: slots of a lane
-  int per;
+  int per[kMaxInputs];
   int wg0[kMaxInputs + 1];
 };
 void plan_heads(const spdp_heads_t* in, int inputs, const spdp_rotation_t* r, long long n_tokens, bool back, int cus, HeadsPlan* p) {
@@ -321,16 +312,21 @@ void plan_heads(const spdp_heads_t* in, int inputs, const spdp_rotation_t* r, lo
   const int groups = 64 / p->lanes;
   long long all = 0, waves = 4ll * cus * kWaves;
   for (int i = 0; i < inputs; ++i) all += n_tokens * in[i].heads;
-  p->per = (int)std::max<long long>(1, std::min<long long>(8, all / (groups * waves)));
+  const long long most_per = std::max<long long>(1, std::min<long long>(8, all / (groups * waves)));
   long long rounds[kMaxInputs], sum = 0;
   for (int i = 0; i < inputs; ++i) {
-    const int chunk = groups * p->per;
+    // equal shares of the heads
+    const long long groups_of = (in[i].heads + groups - 1) / groups;
+    const long long parts = (groups_of + most_per - 1) / most_per;
+    p->per[i] = (int)((groups_of + parts - 1) / parts);
+    const int chunk = groups * p->per[i];
     rounds[i] = n_tokens * ((in[i].heads + chunk - 1) / chunk);
     sum += rounds[i];
   }
-  // backward: each workgroup's share of the weights' gradient is written and
-  // read again, so no more of them than fill the card
-  const long long most = back ? 8ll * cus : 1ll << 30;
+  // backward: each workgroup's share of the weights' gradient is reduced, written
+  // and read again: as many as a CU's registers hold (2048 tokens, 40 + 8 heads of
+  // 96, with 1 / 2 / 3 / 4 per CU: 43 / 34 / 29 / 34 us)
+  const long long most = back ? 3ll * cus : 1ll << 30;
   p->wg0[0] = 0;
   for (int i = 0; i < inputs; ++i) {
     const long long want = (rounds[i] + kWaves - 1) / kWaves;
@@ -358,12 +354,18 @@ int check(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
   return SPDP_OK;
 }
 
-template <int V, int R>
+template <int V, int R, bool PAIRS>
 void launch(const HeadsArgs& a, bool back, dim3 grid, hipStream_t s) {
   if (back)
-    hipLaunchKernelGGL((heads_kernel<V, R, true>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((heads_kernel<V, R, PAIRS, true>), grid, dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((heads_kernel<V, R, false>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((heads_kernel<V, R, PAIRS, false>), grid, dim3(kThreads), 0, s, a);
+}
+template <int V, int R>
+void launch_pairs(const HeadsArgs& a, bool pairs, bool back, dim3 grid, hipStream_t s) {
+  if constexpr (V > 1)
+    if (pairs) return launch<V, R, true>(a, back, grid, s);
+  launch<V, R, false>(a, back, grid, s);
 }
 
 int compute_units(int* cus) {
@@ -435,7 +437,7 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
   }
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   for (int i = 0; i < inputs; ++i) {
-    a.m[i] = HeadsInput{in[i].x, in[i].weight, in[i].dy, in[i].y, nullptr, in[i].heads, p.wg0[i]};
+    a.m[i] = HeadsInput{in[i].x, in[i].weight, in[i].dy, in[i].y, nullptr, in[i].heads, p.wg0[i], p.per[i]};
     if (back && in[i].weight) {
       const int wgs = p.wg0[i + 1] - p.wg0[i];
       a.m[i].part = reinterpret_cast<float*>(ws);
@@ -454,19 +456,18 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
   a.positions = (int)r->table;
   a.dim = r->dim;
   a.half = r->rot / 2;
-  a.interleaved = r->interleaved != 0;
+  const bool pairs = r->interleaved != 0;
   a.lanes = p.lanes;
-  a.per = p.per;
   const dim3 grid((unsigned)p.wg0[inputs]);
   auto s = static_cast<hipStream_t>(stream);
   if (p.v == 8)
-    launch<8, 1>(a, back, grid, s);
+    launch_pairs<8, 1>(a, pairs, back, grid, s);
   else if (p.v == 2 && p.rounds == 1)
-    launch<2, 1>(a, back, grid, s);
+    launch_pairs<2, 1>(a, pairs, back, grid, s);
   else if (p.v == 2)
-    launch<2, 2>(a, back, grid, s);
+    launch_pairs<2, 2>(a, pairs, back, grid, s);
   else
-    launch<1, 4>(a, back, grid, s);
+    launch_pairs<1, 4>(a, pairs, back, grid, s);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && sums > 0) {
     hipLaunchKernelGGL(heads_sum_kernel, dim3((unsigned)((r->dim + 15) / 16), (unsigned)sums), dim3(1024), 0, s, sum);
