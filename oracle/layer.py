@@ -19,8 +19,10 @@ TINY = 2.0 ** -36  # ... and what the second one's last bit is of the largest
 
 
 def half_step(y):
-    """Half a step of fp16 at y: relative 2^-11, absolute 2^-25 below 2^-14."""
-    return np.maximum(2.0 ** -11 * np.abs(y), 2.0 ** -25)
+    """Half a step of fp16 at y: relative 2^-11, absolute 2^-25 below 2^-14;
+    past the largest number (65504) a rounding may give infinity."""
+    y = np.abs(y)
+    return np.where(y > 65504.0, np.inf, np.maximum(2.0 ** -11 * y, 2.0 ** -25))
 
 
 def adapters_of(ids, n, count):

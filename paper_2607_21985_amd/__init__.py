@@ -484,8 +484,8 @@ class Adapters:
 
     ``a`` is fp16 [count, rank, cols], ``b`` fp16 [count, rank, rows] (the
     second factor rank by rank), ``scale`` fp32 [count], all contiguous on one
-    GPU. Nothing is copied: weights that are changed in place count from the
-    next call on.
+    GPU. Nothing is copied: weights that are changed in place, or replaced by
+    others of the same shape, count from the next call on.
 
         y = fp16(base + scale[id] * (x a[id]^T) b[id])
 
@@ -494,20 +494,29 @@ class Adapters:
     """
 
     def __init__(self, a, b, scale):
-        import torch
         if a.dim() != 3 or b.dim() != 3:
             raise ValueError("a and b must be [count, rank, features]")
-        count, rank, cols = a.shape
-        _tensor(a, "a", torch.float16, (count, rank, cols))
-        _tensor(b, "b", torch.float16, (count, rank, b.shape[2]))
-        _tensor(scale, "scale", torch.float32, (count,))
-        _stream(None, (a, b, scale))
         self.a, self.b, self.scale = a, b, scale
-        self.count, self.rank, self.rows, self.cols = count, rank, b.shape[2], cols
-        self._bank = _Bank(a.data_ptr(), b.data_ptr(), scale.data_ptr(), self.rows, cols, count, rank)
+        self.count, self.rank, self.cols = a.shape
+        self.rows = b.shape[2]
+        self._pointers = None
         self._sizes = {}  # workspaces of calls, by their sizes
         need = ctypes.c_size_t()  # checks the sizes
-        _check(lib().spdp_adapt_workspace(ctypes.byref(self._bank), 1, 1, 0, ctypes.byref(need)))
+        _check(lib().spdp_adapt_workspace(ctypes.byref(self._struct()), 1, 1, 0, ctypes.byref(need)))
+
+    def _struct(self) -> _Bank:
+        # the tensors may have been given other memory (``p.data = ...``) or
+        # replaced since the last call
+        at = (self.a.data_ptr(), self.b.data_ptr(), self.scale.data_ptr())
+        if at != self._pointers:
+            import torch
+            _tensor(self.a, "a", torch.float16, (self.count, self.rank, self.cols))
+            _tensor(self.b, "b", torch.float16, (self.count, self.rank, self.rows))
+            _tensor(self.scale, "scale", torch.float32, (self.count,))
+            _stream(None, (self.a, self.b, self.scale))
+            self._bank = _Bank(*at, self.rows, self.cols, self.count, self.rank)
+            self._pointers = at
+        return self._bank
 
     def add_into(self, x, ids, base, y, h=None, stream=None) -> None:
         """Enqueue ``y = base + the adapters' products of x`` for ``x`` [tokens,
@@ -546,7 +555,7 @@ class Adapters:
             some += (ids,)
         s = _stream(stream, some)
         need = ctypes.c_size_t()
-        bank = ctypes.byref(self._bank)
+        bank = ctypes.byref(self._struct())
         _check(lib().spdp_adapt_grad_workspace(bank, n, ids is not None, ctypes.byref(need)))
         ws = _workspace(need.value, x.device, stream)
         _check(lib().spdp_adapt_grad(bank, x.data_ptr(), None if ids is None else ids.data_ptr(), h.data_ptr(),
@@ -580,7 +589,7 @@ def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
         some.append(ids)
     s = _stream(stream, some)
     P = ctypes.c_void_p * k
-    bk = (_Bank * k)(*[m._bank for m in banks])
+    bk = (_Bank * k)(*[m._struct() for m in banks])
     # the size of a workspace depends on nothing but the call's sizes
     key = (n, ids is not None, tuple((m.rows, m.cols, m.rank, m.count) for m in banks[1:]))
     size = banks[0]._sizes.get(key)

@@ -723,6 +723,8 @@ int hip_fail(hipError_t e, const char* what) {
   return fail(SPDP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+constexpr int kLdsPlain = 48 * 1024;  // dynamic LDS that a launch may have without asking
+
 size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 int compute_units(int* cus) {
@@ -816,7 +818,7 @@ int sort_tokens(const int32_t* ids, long long n, int count, const SortPlan& p, u
   *first = reinterpret_cast<int*>(ws + aligned((size_t)n * 4));
   Tile* const tiles = reinterpret_cast<Tile*>(ws + aligned((size_t)n * 4) + aligned((size_t)(count + 2) * 4));
   const int lds = (kSortWaves + 2) * (count + 1) * 4;
-  if (lds > 64 * 1024) {
+  if (lds > kLdsPlain) {
     const hipError_t e =
         hipFuncSetAttribute(reinterpret_cast<const void*>(sort_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute");
@@ -833,7 +835,7 @@ int sort_tokens(const int32_t* ids, long long n, int count, const SortPlan& p, u
 template <int RB, int T>
 hipError_t launch_shrink_form(const ShrinkArgs& a, dim3 grid, hipStream_t st) {
   const int lds = kWaves * T * 16 * RB * 4;
-  if (lds > 64 * 1024) {
+  if (lds > kLdsPlain) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(shrink_kernel<RB, T>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
@@ -858,7 +860,7 @@ template <int RB, int T, bool FUSED>
 hipError_t launch_expand_form(const ExpandArgs& a, dim3 grid, hipStream_t st) {
   constexpr int W = FUSED ? kFusedWaves : kWaves;
   const int lds = ExpandCfg<RB, T, W>::kLds;
-  if (lds > 64 * 1024) {
+  if (lds > kLdsPlain) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(expand_kernel<RB, T, FUSED>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;

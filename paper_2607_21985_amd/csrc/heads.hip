@@ -326,7 +326,7 @@ void plan_heads(const spdp_heads_t* in, int inputs, const spdp_rotation_t* r, lo
   // backward: each workgroup's share of the weights' gradient is reduced, written
   // and read again: as many as a CU's registers hold (2048 tokens, 40 + 8 heads of
   // 96, with 1 / 2 / 3 / 4 per CU: 43 / 34 / 29 / 34 us)
-  const long long most = back ? 3ll * cus : 1ll << 30;
+  const long long most = back ? 3ll * cus : 1ll << 22;
   p->wg0[0] = 0;
   for (int i = 0; i < inputs; ++i) {
     const long long want = (rounds[i] + kWaves - 1) / kWaves;
@@ -409,6 +409,16 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
         return fail(SPDP_ERR_INVALID_ARG, "an output overlaps an input");
       if (i != j && overlap(in[i].y, n, in[j].y, other)) return fail(SPDP_ERR_INVALID_ARG, "outputs overlap");
       if (overlap(in[i].y, n, in[j].weight, (size_t)r->dim * 2)) return fail(SPDP_ERR_INVALID_ARG, "an output overlaps a weight");
+    }
+    if (back && in[i].dweight) {
+      const size_t own = (size_t)r->dim * 4;
+      for (int j = 0; j < inputs; ++j) {
+        const size_t other = row * in[j].heads;
+        if (overlap(in[i].dweight, own, in[j].x, other) || overlap(in[i].dweight, own, in[j].dy, other) ||
+            overlap(in[i].dweight, own, in[j].y, other) || overlap(in[i].dweight, own, in[j].weight, (size_t)r->dim * 2) ||
+            (i != j && overlap(in[i].dweight, own, in[j].dweight, own)))
+          return fail(SPDP_ERR_INVALID_ARG, "a weight's gradient overlaps another array");
+      }
     }
     if (overlap(in[i].y, n, r->positions, (size_t)n_tokens * 4) ||
         overlap(in[i].y, n, r->cosine, (size_t)r->table * r->rot * 2) || overlap(in[i].y, n, r->sine, (size_t)r->table * r->rot * 2))

@@ -152,6 +152,9 @@ expect("gradient without weight", I, rotate_grad([one(dy=Y, dw=1 << 35)]))
 expect("no workspace", I, rotate_grad([one(dy=Y, w=1 << 35, dw=1 << 34)], ws=None))
 expect("small workspace", I, rotate_grad([one(dy=Y, w=1 << 35, dw=1 << 34)], room=4))
 expect("y partly dy", I, rotate_grad([one(dy=OUT + 2)]))
+expect("one gradient for two weights", I, rotate_grad([one(dy=Y, w=1 << 35, dw=1 << 34),
+    one(x=X + (1 << 32), dy=Y, y=OUT + (1 << 32), w=1 << 35, dw=1 << 34)]))
+expect("gradient in x", I, rotate_grad([one(dy=Y, w=1 << 35, dw=X + 16)]))
 """)
 
 
