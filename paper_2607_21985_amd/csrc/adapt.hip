@@ -420,7 +420,14 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = (_Float16)__fmaf_rn(by, sum[e], (float)mybase[p][e]);
       }
-      store8_inside(m.out + row[p] + col, y, left);
+      // (an output that the L2 caches cannot hold does not go through them: 2048
+      // tokens, 28672 wide, 71.5 -> 69 us, 4096 x 4096 28.5 -> 24.5)
+      if (m.stream && left >= 8) {
+        typedef half8 half8_any __attribute__((aligned(2)));
+        __builtin_nontemporal_store(y, reinterpret_cast<half8_any*>(m.out + row[p] + col));
+      } else {
+        store8_inside(m.out + row[p] + col, y, left);
+      }
     }
     wave_fence();
   }
@@ -497,10 +504,10 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
   }
 }
 
-template <int RB>  // 32 RB ranks
-__global__ __launch_bounds__(kThreads) void outer_kernel(OuterArgs a) {
-  constexpr int kRed = 4 * kWaves * 2 * 16 * 64;
-  constexpr int kIn = kWaves * kGroup * kFactorRow;
+template <int RB, int W>  // 32 RB ranks, W waves
+__global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
+  constexpr int kRed = 4 * W * 2 * 16 * 64;
+  constexpr int kIn = W * kGroup * kFactorRow;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kRed > kIn ? kRed : kIn];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -544,17 +551,17 @@ __global__ __launch_bounds__(kThreads) void outer_kernel(OuterArgs a) {
   if (g < groups) {
     places(g);
     request(g);
-    places(g + kWaves);
+    places(g + W);
   }
-  for (; g < groups; g += kWaves) {
+  for (; g < groups; g += W) {
     half8 now[2 * RB];
 #pragma unroll
     for (int p = 0; p < 2; ++p) *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = in[p];
 #pragma unroll
     for (int j = 0; j < 2 * RB; ++j) now[j] = act[j];
-    if (g + kWaves < groups) {
-      request(g + kWaves);
-      places(g + 2 * kWaves);
+    if (g + W < groups) {
+      request(g + W);
+      places(g + 2 * W);
     }
     wave_fence();
 #pragma unroll
@@ -580,13 +587,13 @@ __global__ __launch_bounds__(kThreads) void outer_kernel(OuterArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) red[((wave * 2 + i) * 16 + e) * 64 + lane] = acc[j][i][e];
     __syncthreads();
-    // a wave adds eight of the 32 (block, register) pairs
+    // a wave adds its share of the 32 (block, register) pairs
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int i = q & 1, e = 4 * wave + (q >> 1);
+    for (int q = 0; q < 32 / W; ++q) {
+      const int i = q & 1, e = 16 / W * wave + (q >> 1);
       float sum = red[(i * 16 + e) * 64 + lane];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) sum += red[((w * 2 + i) * 16 + e) * 64 + lane];
+      for (int w = 1; w < W; ++w) sum += red[((w * 2 + i) * 16 + e) * 64 + lane];
       const int r = 32 * j + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
       const int f = f0 + 32 * i + (lane & 31);
       if (r < a.rank && f < m.width) out[(size_t)r * m.width + f] = by * sum;
@@ -753,12 +760,19 @@ Ranges shrink_ranges(int64_t width, long long tiles, int banks, int cus) {
   return {per, (steps + per - 1) / per};
 }
 
-// The pieces that an adapter's tokens are split into: four workgroups of
-// outer_kernel per CU (of three that a CU holds), at least 128 tokens each.
+// The workgroups of outer_kernel without a split, the pieces that an adapter's
+// tokens are split into, and the waves of a workgroup: pieces of many tokens, four
+// workgroups per CU (of three that a CU holds); unsplit, eight waves where there
+// are fewer than two workgroups per CU. Whole backward passes, us, unsplit of
+// four waves / of eight / split: 4096 tokens, 13824 x 5120, rank 64 150 / 154 /
+// 134; 2048, 4096 x 11008, rank 16 64 / 55 / 57; 4000 of 8 adapters, 8192 x 8192,
+// rank 8 106 / 109 / 118.
+long long outer_wgs(const spdp_adapters_t* m) {
+  return ((m->rows + kCols - 1) / kCols + (m->cols + kCols - 1) / kCols) * m->count;
+}
 int outer_splits(const spdp_adapters_t* m, long long n_tokens, int cus) {
-  const long long wgs = ((m->rows + kCols - 1) / kCols + (m->cols + kCols - 1) / kCols) * m->count;
-  const long long want = std::max<long long>(1, 4 * cus / wgs);
-  return (int)std::min<long long>({want, 16, std::max<long long>(1, n_tokens / m->count / 128)});
+  if (n_tokens / m->count <= 2500) return 1;
+  return (int)std::min<long long>(16, std::max<long long>(1, 4 * cus / outer_wgs(m)));
 }
 // and their packed activations: the groups of 16 tokens, one more per piece
 size_t packed_bytes(const spdp_adapters_t* m, long long n_tokens, int splits) {
@@ -905,7 +919,10 @@ hipError_t launch_outer_rb(const OuterArgs& a, int widest, hipStream_t st) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)((widest + kCols - 1) / kCols), (unsigned)a.splits, (unsigned)(2 * a.count));
-  hipLaunchKernelGGL(outer_kernel<RB>, grid, dim3(kThreads), 0, st, a);
+  if (a.waves == 4)
+    hipLaunchKernelGGL((outer_kernel<RB, 4>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((outer_kernel<RB, 8>), grid, dim3(512), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_outer(const OuterArgs& a, int widest, hipStream_t st) {
@@ -981,6 +998,9 @@ void plan_grad(const spdp_adapters_t* m, long long n_tokens, bool ids, int cus, 
   p->bytes = p->sort.bytes + p->part + p->u + p->outer[0] + p->outer[1] + 2 * (p->packed + p->down) + p->most;
 }
 
+// an output larger than the L2 caches (4 MB on each of 8 dies)
+int streams(long long n_tokens, int64_t width) { return n_tokens * width * 2 > 32ll << 20; }
+
 int check_workspace(const void* workspace, size_t have, size_t need) {
   if (need == 0) return SPDP_OK;
   if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
@@ -1051,7 +1071,7 @@ int adapt(const spdp_adapters_t* banks, int32_t n_banks, const uint16_t* const* 
     if (!p.fused) ws += part_bytes(n_tokens, b.rank, p.r[i].splits);
     sa.m[i] = Shrink{X[i], b.a, part, (int)b.cols, p.r[i].per};
     ea.m[i] = Expand{part, b.b, b.scale, base[i], Y[i], H ? H[i] : nullptr, nullptr, nullptr, X[i], b.a,
-                       (int)b.rows, p.fused ? 1 : p.r[i].splits, (int)b.cols};
+                       (int)b.rows, p.fused ? 1 : p.r[i].splits, (int)b.cols, streams(n_tokens, b.rows)};
   }
   hipError_t e = hipSuccess;
   if (!p.fused) e = launch_shrink(sa, p.sort.tile, dim3((unsigned)p.sort.tiles, (unsigned)p.splits, (unsigned)n_banks), s);
@@ -1123,7 +1143,8 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   sa.t = ea.t = t;
   sa.rank = ea.rank = oa.rank = bank->rank;
   sa.m[0] = Shrink{dY, bank->b, part, (int)bank->rows, p.r.per};
-  ea.m[0] = Expand{part, bank->a, bank->scale, base, dX, u, most, H, nullptr, nullptr, (int)bank->cols, p.r.splits, 0};
+  ea.m[0] = Expand{part, bank->a, bank->scale, base, dX, u, most, H, nullptr, nullptr, (int)bank->cols, p.r.splits, 0,
+                   streams(n_tokens, bank->cols)};
   hipError_t e = launch_shrink(sa, p.sort.tile, dim3((unsigned)p.sort.tiles, (unsigned)p.r.splits, 1), s);
   if (e == hipSuccess) e = launch_expand(ea, 1, p.sort, false, cus, s);
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
@@ -1137,6 +1158,7 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   oa.n_tokens = (int)n_tokens;
   oa.count = bank->count;
   oa.splits = p.splits;
+  oa.waves = !split && outer_wgs(bank) < 2 * cus ? 8 : 4;
   e = launch_outer(oa, (int)std::max(bank->rows, bank->cols), s);
   if (e == hipSuccess && split) {
     ReduceArgs ra;

@@ -62,6 +62,7 @@ struct Expand {
   int width;
   int splits;
   int in_width;
+  int stream;  // the output is larger than the caches
 };
 struct ExpandArgs {
   Expand m[kMaxBanks];
@@ -91,6 +92,7 @@ struct OuterArgs {
   int count;
   int rank;
   int splits;
+  int waves;        // of a workgroup of outer_kernel: 4 or 8
 };
 
 }  // namespace spdp_low
