@@ -240,10 +240,12 @@ template <int RB, int T, int W>
 struct ExpandCfg {
   static constexpr int kRank = 16 * RB;
   static constexpr int kActRow = 2 * kRank + 16;  // bytes
-  static constexpr int kWave = kRank * kFactorRow > 4 * T * kOutRow ? kRank * kFactorRow : 4 * T * kOutRow;
+  static constexpr int kPart = RB < 4 ? RB : 4;   // blocks of 16 ranks of the factor that are in LDS at a time
+  static constexpr int kFactor = 16 * kPart * kFactorRow;
+  static constexpr int kWave = kFactor > 4 * T * kOutRow ? kFactor : 4 * T * kOutRow;
   static constexpr int kActs = 32 * kActRow;  // (an MFMA reads 32 rows)
   static constexpr int kLds = 2 * kActs + W * kWave;
-  static_assert(W * T * kRank * 4 <= W * kWave, "the waves' shares of h fit");
+  static_assert(W != kFusedWaves || T * kRank * 4 <= kWave, "the waves' shares of h fit");
 };
 
 template <int RB, int T, bool FUSED>  // 16 RB ranks, tiles of T <= 32 tokens
@@ -272,27 +274,28 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) row[p] = (size_t)tok[8 * p + (lane >> 3)] * m.width;
 
-  // a block's base and factor, requested a block ahead
-  half8 base[kPasses], fac[2 * RB];
-  auto request = [&](int col) __attribute__((always_inline)) {
+  const half8 none = half8{0, 0, 0, 0, 0, 0, 0, 0};
+  // a block's base and factor, the latter by parts, requested a part ahead
+  constexpr int kParts = RB / C::kPart;
+  half8 base[kPasses], fac[2 * C::kPart];
+  auto request = [&](int col, int part) __attribute__((always_inline)) {
     const int left = m.width - col;  // columns of the lane's eight that there are; may be negative
     if (left <= 0) return;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p)
-      if (8 * p + (lane >> 3) < count) base[p] = load8_inside(m.base + row[p] + col, left);
+      if (part == 0 && 8 * p + (lane >> 3) < count) base[p] = load8_inside(m.base + row[p] + col, left);
     if (adapter < 0) return;
 #pragma unroll
-    for (int p = 0; p < 2 * RB; ++p) {
-      const int j = 8 * p + (lane >> 3);
-      if (j < a.rank) fac[p] = load8_inside(factor + (size_t)j * m.width + col, left);
+    for (int p = 0; p < 2 * C::kPart; ++p) {
+      const int j = 16 * C::kPart * part + 8 * p + (lane >> 3);
+      fac[p] = j < a.rank ? load8_inside(factor + (size_t)j * m.width + col, left) : none;
     }
   };
-  const half8 none = half8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) base[p] = none;
 #pragma unroll
-  for (int p = 0; p < 2 * RB; ++p) fac[p] = none;
-  request(first);
+  for (int p = 0; p < 2 * C::kPart; ++p) fac[p] = none;
+  request(first, 0);
 
   float* const red = reinterpret_cast<float*>(lds + 2 * C::kActs);
   if constexpr (FUSED) {
@@ -379,28 +382,33 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
     half8 mybase[kPasses];
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) mybase[p] = base[p];
-    if (adapter >= 0) {
-#pragma unroll
-      for (int p = 0; p < 2 * RB; ++p)
-        *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = left > 0 ? fac[p] : none;
-    }
-    if (b + 1 < a.blocks) request(col + stride);
     float* const sums = reinterpret_cast<float*>(mine);
+    if (adapter < 0 && b + 1 < a.blocks) request(col + stride, 0);
     if (adapter >= 0) {
-      wave_fence();
       float16v acc[2] = {float16v{}, float16v{}};
 #pragma unroll
-      for (int k = 0; k < RB; ++k) {
-        const int at = (lane & 31) * C::kActRow + 2 * (16 * k + 8 * (lane >> 5));
-        const half8 hi = *reinterpret_cast<const half8*>(act_hi + at), lo = *reinterpret_cast<const half8*>(act_lo + at);
+      for (int part = 0; part < kParts; ++part) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const half8 v = read_transposed(mine, kFactorRow, 16 * k, 32 * i);
-          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, v, acc[i], 0, 0, 0);
-          acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, v, acc[i], 0, 0, 0);
+        for (int p = 0; p < 2 * C::kPart; ++p)
+          *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = left > 0 ? fac[p] : none;
+        if (part + 1 < kParts)
+          request(col, part + 1);
+        else if (b + 1 < a.blocks)
+          request(col + stride, 0);
+        wave_fence();
+#pragma unroll
+        for (int k = 0; k < C::kPart; ++k) {
+          const int at = (lane & 31) * C::kActRow + 2 * (16 * (C::kPart * part + k) + 8 * (lane >> 5));
+          const half8 hi = *reinterpret_cast<const half8*>(act_hi + at), lo = *reinterpret_cast<const half8*>(act_lo + at);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const half8 v = read_transposed(mine, kFactorRow, 16 * k, 32 * i);
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, v, acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, v, acc[i], 0, 0, 0);
+          }
         }
+        wave_fence();
       }
-      wave_fence();
       // register e: token 8 (e / 4) + 4 (lane / 32) + e mod 4, column lane mod 32
 #pragma unroll
       for (int i = 0; i < 2; ++i)
