@@ -92,7 +92,7 @@ __device__ __forceinline__ void shrink_steps(const uint16_t* in, const uint16_t*
                                              int s0, int s1, float* red) {
   constexpr int TB = T / 16;
   // halves of a step that are loaded at once, the next ones during their MFMAs
-  constexpr int D = RB * TB <= 2 ? 4 : RB * TB <= 4 ? 2 : 1;
+  constexpr int D = RB + TB <= 5 ? 4 : RB + TB <= 10 ? 2 : 1;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // four lanes have a row's 64 columns, 16 of them each: 128 bytes of a row at
