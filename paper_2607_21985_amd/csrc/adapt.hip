@@ -512,24 +512,29 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
   }
 }
 
-template <int RB, int W>  // 32 RB ranks, W waves
+template <int RB, int W, int FB>  // 32 RB ranks, W waves, 32 FB columns
 __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
+  constexpr int kRow = 64 * FB + 16;  // bytes of a token's columns in LDS, padded
+  constexpr int kRowLanes = 4 * FB;   // lanes that load a token's columns
+  constexpr int kRows = 64 / kRowLanes;
   constexpr int kRed = 4 * W * 2 * 16 * 64;
-  constexpr int kIn = W * kGroup * kFactorRow;
+  constexpr int kIn = W * kGroup * kRow;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kRed > kIn ? kRed : kIn];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int which = (int)blockIdx.z / a.count, adapter = (int)blockIdx.z % a.count;
   const Outer& m = a.m[which];
-  const int f0 = (int)blockIdx.x * kCols;
+  const int f0 = (int)blockIdx.x * 32 * FB;
   if (f0 >= m.width) return;
   const Piece piece = piece_of(a, adapter, blockIdx.y);
 
-  float16v acc[RB][2];
+  float16v acc[RB][FB];
 #pragma unroll
-  for (int j = 0; j < RB; ++j) acc[j][0] = acc[j][1] = float16v{};
-  unsigned char* const mine = lds + wave * kGroup * kFactorRow;
-  const int col = f0 + 8 * (lane & 7);
+  for (int j = 0; j < RB; ++j)
+#pragma unroll
+    for (int i = 0; i < FB; ++i) acc[j][i] = float16v{};
+  unsigned char* const mine = lds + wave * kGroup * kRow;
+  const int col = f0 + 8 * (lane % kRowLanes);
   const int left = m.width - col;
   const half8* const packed = reinterpret_cast<const half8*>(m.packed) + piece.group0 * RB * 128 + lane;
   const int groups = (piece.t1 - piece.t0 + kGroup - 1) / kGroup;
@@ -537,18 +542,18 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
 
   // a group's input and operands, requested a group ahead, its tokens' places
   // two ahead
-  int at[2];
-  half8 in[2], act[2 * RB];
+  int at[FB];
+  half8 in[FB], act[2 * RB];
   auto places = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int t = piece.t0 + g * kGroup + 8 * p + (lane >> 3);
+    for (int p = 0; p < FB; ++p) {
+      const int t = piece.t0 + g * kGroup + kRows * p + lane / kRowLanes;
       at[p] = t < piece.t1 ? (a.perm ? a.perm[t] : t) : -1;
     }
   };
   auto request = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < FB; ++p) {
       in[p] = none;
       if (at[p] >= 0 && left > 0) in[p] = load8_inside(m.in + (size_t)at[p] * m.width + col, left);
     }
@@ -564,7 +569,8 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
   for (; g < groups; g += W) {
     half8 now[2 * RB];
 #pragma unroll
-    for (int p = 0; p < 2; ++p) *reinterpret_cast<half8*>(mine + (8 * p + (lane >> 3)) * kFactorRow + 16 * (lane & 7)) = in[p];
+    for (int p = 0; p < FB; ++p)
+      *reinterpret_cast<half8*>(mine + (kRows * p + lane / kRowLanes) * kRow + 16 * (lane % kRowLanes)) = in[p];
 #pragma unroll
     for (int j = 0; j < 2 * RB; ++j) now[j] = act[j];
     if (g + W < groups) {
@@ -573,8 +579,8 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
     }
     wave_fence();
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const half8 v = read_transposed(mine, kFactorRow, 0, 32 * i);
+    for (int i = 0; i < FB; ++i) {
+      const half8 v = read_transposed(mine, kRow, 0, 32 * i);
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
         acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[2 * j], v, acc[j][i], 0, 0, 0);
@@ -585,28 +591,30 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
   }
 
   const float by = m.down[piece.index] * a.scale[adapter];
-  float* const red = reinterpret_cast<float*>(lds);  // [wave][column block][register][lane]
+  float* const red = reinterpret_cast<float*>(lds);  // [wave][two column blocks][register][lane]
   float* const out = m.out + ((size_t)blockIdx.y * a.count + adapter) * a.rank * m.width;
 #pragma unroll
-  for (int j = 0; j < RB; ++j) {
-    __syncthreads();
+  for (int j = 0; j < RB; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i0 = 0; i0 < FB; i0 += 2) {
+      __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 16; ++e) red[((wave * 2 + i) * 16 + e) * 64 + lane] = acc[j][i][e];
-    __syncthreads();
-    // a wave adds its share of the 32 (block, register) pairs
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int q = 0; q < 32 / W; ++q) {
-      const int i = q & 1, e = 16 / W * wave + (q >> 1);
-      float sum = red[(i * 16 + e) * 64 + lane];
+        for (int e = 0; e < 16; ++e) red[((wave * 2 + i) * 16 + e) * 64 + lane] = acc[j][i0 + i][e];
+      __syncthreads();
+      // a wave adds its share of the 32 (block, register) pairs
 #pragma unroll
-      for (int w = 1; w < W; ++w) sum += red[((w * 2 + i) * 16 + e) * 64 + lane];
-      const int r = 32 * j + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
-      const int f = f0 + 32 * i + (lane & 31);
-      if (r < a.rank && f < m.width) out[(size_t)r * m.width + f] = by * sum;
+      for (int q = 0; q < 32 / W; ++q) {
+        const int i = q & 1, e = 16 / W * wave + (q >> 1);
+        float sum = red[(i * 16 + e) * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w) sum += red[((w * 2 + i) * 16 + e) * 64 + lane];
+        const int r = 32 * j + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+        const int f = f0 + 32 * (i0 + i) + (lane & 31);
+        if (r < a.rank && f < m.width) out[(size_t)r * m.width + f] = by * sum;
+      }
     }
-  }
 }
 
 struct ReduceArgs {
@@ -775,12 +783,32 @@ Ranges shrink_ranges(int64_t width, long long tiles, int banks, int cus) {
 // four waves / of eight / split: 4096 tokens, 13824 x 5120, rank 64 150 / 154 /
 // 134; 2048, 4096 x 11008, rank 16 64 / 55 / 57; 4000 of 8 adapters, 8192 x 8192,
 // rank 8 106 / 109 / 118.
-long long outer_wgs(const spdp_adapters_t* m) {
-  return ((m->rows + kCols - 1) / kCols + (m->cols + kCols - 1) / kCols) * m->count;
+//
+// Much input and ranks up to 64: 128 columns, which read the packed activations
+// half as often (they come from L2, twice the input's bytes at rank 64 and 64
+// columns), and the pieces that fill the two workgroups that a CU holds best
+// (4096 tokens, 13824 x 5120, rank 64 132 -> 124 us; 16384, 4096 x 4096, rank 16
+// 169 -> 158; 3000, 11008 x 4096, rank 32 would take 79 for 76).
+long long outer_wgs(const spdp_adapters_t* m, int cols) {
+  return ((m->rows + cols - 1) / cols + (m->cols + cols - 1) / cols) * m->count;
+}
+bool outer_wide(const spdp_adapters_t* m, long long n_tokens) {
+  return m->rank <= 64 && n_tokens / m->count > 2500 && n_tokens * (m->rows + m->cols) > 70000000;
 }
 int outer_splits(const spdp_adapters_t* m, long long n_tokens, int cus) {
   if (n_tokens / m->count <= 2500) return 1;
-  return (int)std::min<long long>(16, std::max<long long>(1, 4 * cus / outer_wgs(m)));
+  if (!outer_wide(m, n_tokens)) return (int)std::min<long long>(16, std::max<long long>(1, 4 * cus / outer_wgs(m, kCols)));
+  int best = 1;
+  float most = 0.0f;
+  for (int s = 1; s <= 8; ++s) {
+    const long long wgs = outer_wgs(m, 2 * kCols) * s, slots = 2ll * cus;
+    const float fill = (float)wgs / (float)((wgs + slots - 1) / slots * slots) - 0.05f * (float)s;
+    if (fill > most) {
+      most = fill;
+      best = s;
+    }
+  }
+  return best;
 }
 // and their packed activations: the groups of 16 tokens, one more per piece
 size_t packed_bytes(const spdp_adapters_t* m, long long n_tokens, int splits) {
@@ -926,11 +954,15 @@ hipError_t launch_outer_rb(const OuterArgs& a, int widest, hipStream_t st) {
   hipLaunchKernelGGL(pack_kernel<RB>, dim3(share, (unsigned)a.splits, (unsigned)(2 * a.count)), dim3(kThreads), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)((widest + kCols - 1) / kCols), (unsigned)a.splits, (unsigned)(2 * a.count));
-  if (a.waves == 4)
-    hipLaunchKernelGGL((outer_kernel<RB, 4>), grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((outer_kernel<RB, 8>), grid, dim3(512), 0, st, a);
+  const int cols = a.wide ? 2 * kCols : kCols;
+  const dim3 grid((unsigned)((widest + cols - 1) / cols), (unsigned)a.splits, (unsigned)(2 * a.count));
+  if (a.wide) {
+    if constexpr (RB <= 2) hipLaunchKernelGGL((outer_kernel<RB, 4, 4>), grid, dim3(256), 0, st, a);
+  } else if (a.waves == 4) {
+    hipLaunchKernelGGL((outer_kernel<RB, 4, 2>), grid, dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((outer_kernel<RB, 8, 2>), grid, dim3(512), 0, st, a);
+  }
   return hipGetLastError();
 }
 hipError_t launch_outer(const OuterArgs& a, int widest, hipStream_t st) {
@@ -1166,7 +1198,8 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   oa.n_tokens = (int)n_tokens;
   oa.count = bank->count;
   oa.splits = p.splits;
-  oa.waves = !split && outer_wgs(bank) < 2 * cus ? 8 : 4;
+  oa.wide = outer_wide(bank, n_tokens);
+  oa.waves = !split && outer_wgs(bank, kCols) < 2 * cus ? 8 : 4;
   e = launch_outer(oa, (int)std::max(bank->rows, bank->cols), s);
   if (e == hipSuccess && split) {
     ReduceArgs ra;

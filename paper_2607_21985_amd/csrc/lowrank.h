@@ -93,6 +93,7 @@ struct OuterArgs {
   int rank;
   int splits;
   int waves;        // of a workgroup of outer_kernel: 4 or 8
+  int wide;         // 128 columns instead of 64
 };
 
 }  // namespace spdp_low

@@ -60,6 +60,43 @@ def test_adapters_beyond_32_bits():
     assert torch.all((db[2, :, -8:].double() - want).abs() <= (layer.SPLIT + 2 * own.numel() * layer.U32) * size)
 
 
+@pytest.mark.parametrize("ids", [False, True])
+@pytest.mark.parametrize("n,rows,cols,rank", [(9001, 5003, 3081, 40), (5100, 9000, 6000, 7), (2600, 4100, 777, 64)])
+def test_gradients_of_many_tokens(n, rows, cols, rank, ids):
+    # against float64 on the GPU, with the oracle's bounds
+    torch.manual_seed(n + rank)
+    count = 2 if ids else 1
+    x, dy, base = _filled(n, cols), _filled(n, rows, 0.1), _filled(n, cols)
+    a, b = (0.1 * torch.randn(count, rank, w, device="cuda").half() for w in (cols, rows))
+    scale, h = torch.rand(count, device="cuda") + 0.5, torch.randn(n, rank, device="cuda")
+    which = torch.randint(-1, 2, (n,), device="cuda", dtype=torch.int32) if ids else None
+    m = spdp.Adapters(a, b, scale)
+    dx, da, db = torch.empty_like(x), torch.empty(a.shape, device="cuda"), torch.empty(b.shape, device="cuda")
+    m.grad_into(x, which, h, dy, base, dx, da, db)
+    for i in range(count):
+        at = torch.arange(n, device="cuda") if which is None else torch.nonzero(which == i).flatten()
+        s, k = float(scale[i]), at.numel()
+        z, g, act = x[at].double(), dy[at].double(), h[at].double()
+        bt = b[i].double().t().contiguous()
+        u = g @ bt
+        ue = 2 * rows * layer.U32 * (g.abs() @ bt.abs())
+        per = layer.SPLIT + 2 * (2 * k + 2) * layer.U32
+        for got, v, ve, t in ((da[i], u, ue, z), (db[i], act, torch.zeros_like(act), g)):
+            want = s * (v.t().contiguous() @ t)
+            size = v.abs() + ve
+            bound = s * ((ve + per * size + layer.TINY * size.max()).t().contiguous() @ t.abs()) + 4 * layer.U32 * want.abs()
+            assert torch.all((got.double() - want).abs() <= bound)
+        want = base[at].double() + s * (u @ a[i].double())
+        size = u.abs() + ue
+        part = ue + (layer.SPLIT + 2 * (2 * rank + 2) * layer.U32) * size + layer.TINY * size.amax(1, keepdim=True)
+        bound = s * (part @ a[i].double().abs()) + 4 * layer.U32 * want.abs()
+        bound += torch.clamp(2.0 ** -11 * (want.abs() + bound), min=2.0 ** -25)
+        assert torch.all((dx[at].double() - want).abs() <= bound)
+    if which is not None:
+        none = which < 0
+        assert torch.equal(dx[none], base[none])
+
+
 def test_heads_beyond_32_bits():
     n, heads, dim = 140_000, 128, 128
     assert n * heads * dim > 1 << 31
