@@ -98,11 +98,3 @@ struct WideLaunch {
 
 // Launches the all-columns form for `batch` tokens.
 hipError_t launch_wide(const WideLaunch& args, int count, bool bmask, dim3 grid, hipStream_t stream);
-
-namespace spdp {
-
-// y = fp16(part[0] + part[1] + ...), `splits` arrays of `count` sums added in
-// order (spmm.hip).
-hipError_t launch_reduce(const float* part, int splits, long long count, uint16_t* y, hipStream_t stream);
-
-}  // namespace spdp

@@ -34,7 +34,6 @@
 
 #include "expand.h"
 #include "internal.h"
-#include "launch.h"
 
 namespace {
 
@@ -1134,13 +1133,6 @@ hipError_t launch_rows(const RowArgs& a, int tb, bool xv, bool fold, dim3 grid, 
 
 }  // namespace
 
-hipError_t spdp::launch_reduce(const float* part, int splits, long long count, uint16_t* y, hipStream_t stream) {
-  const long long per = (count & 3) == 0 ? count / 4 : count;
-  const unsigned blocks = (unsigned)std::min<long long>(8192, (per + 255) / 256);
-  hipLaunchKernelGGL(spmm_reduce_kernel, dim3(blocks), dim3(256), 0, stream, part, splits, count, y);
-  return hipGetLastError();
-}
-
 extern "C" int spdp_spmm(spdp_handle_t h, const uint16_t* X, int64_t n_tokens, uint16_t* Y, void* stream) {
   using spdp::fail;
   spdp::clear_error();
@@ -1235,7 +1227,13 @@ extern "C" int spdp_spmm(spdp_handle_t h, const uint16_t* X, int64_t n_tokens, u
     e = hipGetLastError();
   }
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
-  if (part) e = spdp::launch_reduce(part, plan.splits, n_tokens * h->rows, Y, st);
+  if (part) {
+    const long long count = n_tokens * h->rows;
+    const long long per = (count & 3) == 0 ? count / 4 : count;
+    const unsigned blocks = (unsigned)std::min<long long>(8192, (per + 255) / 256);
+    hipLaunchKernelGGL(spmm_reduce_kernel, dim3(blocks), dim3(256), 0, st, part, plan.splits, count, Y);
+  }
+  e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return SPDP_OK;
 }

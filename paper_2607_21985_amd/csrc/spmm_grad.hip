@@ -18,7 +18,6 @@
 
 #include "internal.h"
 #include "lanes.h"
-#include "launch.h"
 
 namespace {
 
@@ -375,6 +374,27 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
   for (int t = 0; t < TB; ++t) store_sums(a, acc[t], nb0 + 32 * (TB * tg + t), col);
 }
 
+// dX = fp16(sum over the ranges of part[z]), added in order, so that the result
+// does not depend on timing; V outputs a lane (4 where the count divides).
+template <int V>
+__global__ __launch_bounds__(kThreads) void grad_reduce_kernel(const float* __restrict__ part, int splits, long long count,
+                                                               uint16_t* __restrict__ dx) {
+  typedef float floats __attribute__((ext_vector_type(V)));
+  const long long stride = (long long)gridDim.x * kThreads;
+  for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < count / V; i += stride) {
+    floats sum = reinterpret_cast<const floats*>(part)[i];
+#pragma unroll 4
+    for (int z = 1; z < splits; ++z) sum += reinterpret_cast<const floats*>(part + (size_t)z * (size_t)count)[i];
+    uint16_t h[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float v = sum[e];
+      h[e] = __half_as_ushort(__float2half_rn(v));
+    }
+    __builtin_memcpy(dx + V * i, h, 2 * V);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Host side.
 
@@ -553,8 +573,16 @@ int spmm_grad(spdp_handle_t h, const uint16_t* dY, int64_t n_tokens, uint16_t* d
     hipLaunchKernelGGL(grad_plain_kernel, grid, dim3(kThreads), 0, s, a);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && p.splits > 1)
-    e = spdp::launch_reduce(a.part, p.splits, n_tokens * h->cols, dX, s);
+  if (e == hipSuccess && p.splits > 1) {
+    const long long count = n_tokens * h->cols;
+    const bool four = count % 4 == 0;
+    const unsigned wgs = (unsigned)std::min<long long>(8192, ((four ? count / 4 : count) + kThreads - 1) / kThreads);
+    if (four)
+      hipLaunchKernelGGL(grad_reduce_kernel<4>, dim3(wgs), dim3(kThreads), 0, s, a.part, p.splits, count, dX);
+    else
+      hipLaunchKernelGGL(grad_reduce_kernel<1>, dim3(wgs), dim3(kThreads), 0, s, a.part, p.splits, count, dX);
+    e = hipGetLastError();
+  }
   return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");
 }
 
