@@ -923,7 +923,8 @@ hipError_t launch_expand_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_
   return tile == 16 ? launch_expand_form<RB, 16, false>(a, grid, st) : launch_expand_form<RB, 32, false>(a, grid, st);
 }
 hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused, int cus, hipStream_t st) {
-  // (64 tokens of a workgroup of expand_kernel took 1.2 to 3.4 times as long)
+  // (with 64 tokens a workgroup of expand_kernel is slower: 65 us for 56 of 2048
+  // tokens of rank 32, 28672 wide, 33 for 30 of 4096 of rank 64, 5120 wide)
   a.subs = p.tile > 32 ? p.tile / 32 : 1;
   const long long tiles = p.tiles * a.subs;
   int widest = 0;
