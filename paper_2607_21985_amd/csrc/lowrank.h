@@ -94,6 +94,7 @@ struct OuterArgs {
   int splits;
   int waves;        // of a workgroup of outer_kernel: 4 or 8
   int wide;         // 128 columns instead of 64
+  int packed;       // the activations are
 };
 
 }  // namespace spdp_low

@@ -203,6 +203,8 @@ assert adapt(n=500, ids=None, y=[BASE], h=[H]) == 0
 out["one adapter"] = names()
 assert grad(n=4, dx=BASE) == 0
 out["grad"] = names()
+assert grad(n=300) == 0
+out["grad of 300"] = names()
 assert grad(bank(count=1), n=4096, ids=None) == 0
 out["grad of many tokens"] = names()
 assert rotate([one(y=X), one(x=Y, y=Y + (1 << 30))]) == 0
@@ -223,7 +225,8 @@ for n in (1, 31, 64, 65, 1000, 5000, 1 << 20):
     assert out["one token"] == ["expand"]
     assert out["a large first factor"] == out["64"] == out["one adapter"] == ["shrink", "expand"]
     assert out["65"] == ["sort", "shrink", "expand"]
-    assert out["grad"] == ["sort", "shrink", "expand", "pack", "outer"]
+    assert out["grad"] == ["sort", "shrink", "expand", "outer"]
+    assert out["grad of 300"] == ["sort", "shrink", "expand", "pack", "outer"]
     assert out["grad of many tokens"] == ["shrink", "expand", "pack", "outer", "outer_reduce"]
     assert out["heads"] == out["heads grad without weights"] == ["heads"]
     assert out["heads grad"] == ["heads", "heads_sum"]
