@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -105,6 +106,15 @@ class _Rotation(ctypes.Structure):
 class _Heads(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("dy", ctypes.c_void_p),
                 ("y", ctypes.c_void_p), ("dweight", ctypes.c_void_p), ("heads", ctypes.c_int32)]
+
+
+# the same layouts as bytes, which small calls build in a fraction of the time
+_PACK_BANK = struct.Struct("PPPqqii")
+_PACK_ROTATION = struct.Struct("PPPqiiif")
+_PACK_HEADS = struct.Struct("PPPPPi4x")
+_PACK_POINTERS = [struct.Struct(f"{_k}P").pack for _k in range(9)]
+for _a, _b in ((_PACK_BANK, _Bank), (_PACK_ROTATION, _Rotation), (_PACK_HEADS, _Heads)):
+    assert _a.size == ctypes.sizeof(_b)
 
 
 _lib = None
@@ -502,9 +512,9 @@ class Adapters:
         self._pointers = None
         self._sizes = {}  # workspaces of calls, by their sizes
         need = ctypes.c_size_t()  # checks the sizes
-        _check(lib().spdp_adapt_workspace(ctypes.byref(self._struct()), 1, 1, 0, ctypes.byref(need)))
+        _check(lib().spdp_adapt_workspace(self._struct(), 1, 1, 0, ctypes.byref(need)))
 
-    def _struct(self) -> _Bank:
+    def _struct(self) -> bytes:
         # the tensors may have been given other memory (``p.data = ...``) or
         # replaced since the last call
         at = (self.a.data_ptr(), self.b.data_ptr(), self.scale.data_ptr())
@@ -514,7 +524,7 @@ class Adapters:
             _tensor(self.b, "b", torch.float16, (self.count, self.rank, self.rows))
             _tensor(self.scale, "scale", torch.float32, (self.count,))
             _stream(None, (self.a, self.b, self.scale))
-            self._bank = _Bank(*at, self.rows, self.cols, self.count, self.rank)
+            self._bank = _PACK_BANK.pack(*at, self.rows, self.cols, self.count, self.rank)
             self._pointers = at
         return self._bank
 
@@ -555,7 +565,7 @@ class Adapters:
             some += (ids,)
         s = _stream(stream, some)
         need = ctypes.c_size_t()
-        bank = ctypes.byref(self._struct())
+        bank = self._struct()
         _check(lib().spdp_adapt_grad_workspace(bank, n, ids is not None, ctypes.byref(need)))
         ws = _workspace(need.value, x.device, stream)
         _check(lib().spdp_adapt_grad(bank, x.data_ptr(), None if ids is None else ids.data_ptr(), h.data_ptr(),
@@ -572,14 +582,16 @@ def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
     if not (len(xs) == len(bases) == len(ys) == k) or (hs is not None and len(hs) != k) or k == 0:
         raise ValueError("banks, xs, bases, ys and hs must have one entry per projection")
     f16, n, L = torch.float16, xs[0].shape[0], lib()
-    some = [m.a for m in banks]
-    some += xs
-    some += bases
-    some += ys
+    some = [*xs, *bases, *ys]
+    bk, key = [], [n, ids is not None]
     for m, x, base, y in zip(banks, xs, bases, ys):
+        bk.append(m._struct())
+        some.append(m.a)
+        key += (m.rows, m.cols, m.rank, m.count)
         _tensor(x, "x", f16, (n, m.cols))
-        _tensor(base, "base", f16, (n, m.rows))
-        _tensor(y, "y", f16, (n, m.rows))
+        out = (n, m.rows)
+        _tensor(base, "base", f16, out)
+        _tensor(y, "y", f16, out)
     if hs is not None:
         for m, h in zip(banks, hs):
             _tensor(h, "h", torch.float32, (n, m.rank))
@@ -588,64 +600,65 @@ def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
         _tensor(ids, "ids", torch.int32, (n,))
         some.append(ids)
     s = _stream(stream, some)
-    P = ctypes.c_void_p * k
-    bk = (_Bank * k)(*[m._struct() for m in banks])
+    bk = b"".join(bk)
     # the size of a workspace depends on nothing but the call's sizes
-    key = (n, ids is not None, tuple((m.rows, m.cols, m.rank, m.count) for m in banks[1:]))
-    size = banks[0]._sizes.get(key)
+    sizes, key = banks[0]._sizes, tuple(key)
+    size = sizes.get(key)
     if size is None:
         need = ctypes.c_size_t()
         _check(L.spdp_adapt_workspace(bk, k, n, ids is not None, ctypes.byref(need)))
-        if len(banks[0]._sizes) >= 256:
-            banks[0]._sizes.clear()
-        banks[0]._sizes[key] = size = need.value
-    ws = _workspace(size, xs[0].device, stream)
+        if len(sizes) >= 256:
+            sizes.clear()
+        sizes[key] = size = need.value
+    ws = _workspace(size, xs[0].device, stream) if size else None
+    P = _PACK_POINTERS[k] if k < len(_PACK_POINTERS) else struct.Struct(f"{k}P").pack
     _check(L.spdp_adapt(bk, k, P(*[x.data_ptr() for x in xs]), None if ids is None else ids.data_ptr(),
                         P(*[b.data_ptr() for b in bases]), P(*[y.data_ptr() for y in ys]),
-                        None if hs is None else P(*[h.data_ptr() for h in hs]), n, ws.data_ptr(), size, s))
+                        None if hs is None else P(*[h.data_ptr() for h in hs]), n, ws.data_ptr() if size else None, size, s))
 
 
 def _heads(xs, dim, pos, cos, sin, ys, weights, eps, interleaved, stream, dys=None, dweights=None):
     import torch
     k = len(xs)
-    if k == 0 or len(ys) != k or any(v is not None and len(v) != k for v in (weights, dys, dweights)):
+    if k == 0 or len(ys) != k or (weights is not None and len(weights) != k) or (dys is not None and len(dys) != k) or \
+            (dweights is not None and len(dweights) != k):
         raise ValueError("every list must have one entry per input")
     if dim < 1:
         raise ValueError("dim must be at least 1")
-    f16, n = torch.float16, xs[0].shape[0]
+    f16, f32, n = torch.float16, torch.float32, xs[0].shape[0]
     _tensor(pos, "pos", torch.int32, (n,))
-    if cos.dim() != 2:
+    angles = cos.shape
+    if len(angles) != 2:
         raise ValueError("cos and sin must be [positions, rot / 2]")
-    _tensor(cos, "cos", torch.float32, cos.shape)
-    _tensor(sin, "sin", torch.float32, cos.shape)
-    some = [pos, cos, sin]
-    some += xs
-    some += ys
+    _tensor(cos, "cos", f32, angles)
+    _tensor(sin, "sin", f32, angles)
+    some = [pos, cos, sin, *xs, *ys]
     inputs = []
-    for i, (x, y) in enumerate(zip(xs, ys)):
-        if x.dim() != 2 or x.shape[1] % dim or x.shape[1] == 0:
-            raise ValueError(f"x must be [tokens, heads * {dim}]")
-        width = x.shape[1]
-        _tensor(x, "x", f16, (n, width))
-        _tensor(y, "the output", f16, (n, width))
-        w = d = dw = None
+    for i in range(k):
+        x, y = xs[i], ys[i]
+        shape = x.shape
+        if len(shape) != 2 or shape[0] != n or shape[1] % dim or shape[1] == 0:
+            raise ValueError(f"x must be [{n}, heads * {dim}]")
+        _tensor(x, "x", f16, shape)
+        _tensor(y, "the output", f16, shape)
+        w = d = dw = 0
         if weights is not None and weights[i] is not None:
             _tensor(weights[i], "a weight", f16, (dim,))
             some.append(weights[i])
             w = weights[i].data_ptr()
         if dys is not None:
-            _tensor(dys[i], "dy", f16, (n, width))
+            _tensor(dys[i], "dy", f16, shape)
             some.append(dys[i])
             d = dys[i].data_ptr()
         if dweights is not None and dweights[i] is not None:
-            _tensor(dweights[i], "a weight's gradient", torch.float32, (dim,))
+            _tensor(dweights[i], "a weight's gradient", f32, (dim,))
             some.append(dweights[i])
             dw = dweights[i].data_ptr()
-        inputs.append(_Heads(x.data_ptr(), w, d, y.data_ptr(), dw, width // dim))
+        inputs.append(_PACK_HEADS.pack(x.data_ptr(), w, d, y.data_ptr(), dw, shape[1] // dim))
     s = _stream(stream, some)
-    table, half = cos.shape
-    r = _Rotation(pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), table, dim, 2 * half, 1 if interleaved else 0, eps)
-    return (_Heads * k)(*inputs), k, ctypes.byref(r), n, s
+    r = _PACK_ROTATION.pack(pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), angles[0], dim, 2 * angles[1],
+                            1 if interleaved else 0, eps)
+    return b"".join(inputs), k, r, n, s
 
 
 def rotate_heads(xs, dim, pos, cos, sin, ys, weights=None, eps=1e-6, interleaved=False, stream=None) -> None:
