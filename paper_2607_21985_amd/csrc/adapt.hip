@@ -957,6 +957,10 @@ template <int RB>
 hipError_t launch_expand_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_t st) {
   return tile == 16 ? launch_expand_form<RB, 16, false>(a, grid, st) : launch_expand_form<RB, 32, false>(a, grid, st);
 }
+template <int RB>
+hipError_t launch_fused_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_t st) {
+  return tile == 16 ? launch_expand_form<RB, 16, true>(a, grid, st) : launch_expand_form<RB, 32, true>(a, grid, st);
+}
 hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused, int cus, hipStream_t st) {
   // (with 64 tokens a workgroup of expand_kernel is slower: 65 us for 56 of 2048
   // tokens of rank 32, 28672 wide, 33 for 30 of 4096 of rank 64, 5120 wide)
@@ -974,9 +978,9 @@ hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused
   a.blocks = (int)std::max<long long>(1, std::min<long long>(5, (blocks * tiles * banks + fill - 1) / fill));
   const dim3 grid((unsigned)((blocks + a.blocks - 1) / a.blocks), (unsigned)tiles, (unsigned)banks);
   if (fused)
-    return a.rank <= 16   ? launch_expand_form<1, 16, true>(a, grid, st)
-           : a.rank <= 32 ? launch_expand_form<2, 16, true>(a, grid, st)
-                          : launch_expand_form<4, 16, true>(a, grid, st);
+    return a.rank <= 16   ? launch_fused_rb<1>(a, p.tile, grid, st)
+           : a.rank <= 32 ? launch_fused_rb<2>(a, p.tile, grid, st)
+                          : launch_fused_rb<4>(a, p.tile, grid, st);
   if (a.rank <= 16) return launch_expand_rb<1>(a, p.tile, grid, st);
   if (a.rank <= 32) return launch_expand_rb<2>(a, p.tile, grid, st);
   if (a.rank <= 64) return launch_expand_rb<4>(a, p.tile, grid, st);
@@ -1040,13 +1044,14 @@ void plan_adapt(const spdp_adapters_t* banks, int n_banks, long long n_tokens, b
   // The fused form, where a workgroup's own pass over the first factor (at 16,
   // 32 or 64 ranks) is short and the workgroups that make it are few. Two
   // launches -> fused, us per pass, called in sequence and from a graph: one
-  // token of rank 8, 1024 wide, 11.4 / 7.0 -> 8.7 / 5.1; 16 requests of rank 16,
-  // three 4096 wide, 12.9 / 9.7 -> 10.7 / 10.5; 32 of them 12.8 / 11.9 -> 16.7 /
-  // 17.1; one of rank 32, three 4096 wide, 13.0 / 9.2 -> 13.0 / 12.9.
+  // token of rank 8, 1024 wide, 11.4 / 7.0 -> 8.7 / 5.1; 24 of 5 adapters of rank
+  // 12, 5003 x 3080, 10.9 / 8.4 -> 8.2 / 8.1; one of rank 16, 4096 wide, 10.9 / 7.6
+  // -> 9.0 / 8.8; 333 of 4 adapters of rank 16, 1024 wide (and the sort) 13.9 /
+  // 13.5 -> 12.2 / 12.1, 4096 wide 15.1 / 14.2 -> 20.8 / 20.9.
   long long wgs = 0;
-  p->fused = !p->sort.sorted && p->sort.tile == 16 && banks[0].rank <= 64;
+  p->fused = p->sort.tile <= 32 && banks[0].rank <= 64;
   for (int i = 0; i < n_banks; ++i) {
-    p->fused = p->fused && (banks[i].rank + 15) / 16 * 16 * banks[i].cols <= 1 << 16;
+    p->fused = p->fused && (banks[i].rank + 15) / 16 * 16 * banks[i].cols <= (p->sort.tile == 16 ? 50000 : 20000);
     wgs += p->sort.tiles * ((banks[i].rows + kCols * kFusedWaves - 1) / (kCols * kFusedWaves));
   }
   p->fused = p->fused && 2 * wgs <= 3 * cus;

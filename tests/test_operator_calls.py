@@ -87,7 +87,7 @@ expect("tokens", U, adapt(n=(1 << 20) + 1, room=1 << 30))
 expect("null entry", I, adapt(x=[None]))
 expect("null output", I, adapt(y=[None]))
 expect("null h", I, adapt(h=[None]))
-expect("no workspace", I, adapt(n=200, ws=None))
+expect("no workspace", I, adapt([bank(cols=4096)], n=200, ws=None))
 expect("small workspace", I, adapt(n=200, room=need([bank()], 200)[1] - 1))
 expect("odd workspace", I, adapt(n=200, ws=WS + 128))
 expect("Y in X", I, adapt(y=[X + 40 * 128 * 2 - 2]))
@@ -196,10 +196,14 @@ out["one token"] = names()
 assert adapt([bank(cols=8192, rank=32)], n=1) == 0
 out["a large first factor"] = names()
 assert adapt([bank(count=1)], n=64) == 0
+out["64 of one adapter"] = names()
+assert adapt([bank(cols=4096, count=1)], n=64) == 0
 out["64"] = names()
 assert adapt(n=65) == 0
 out["65"] = names()
-assert adapt(n=500, ids=None, y=[BASE], h=[H]) == 0
+assert adapt([bank(cols=4096)], n=65) == 0
+out["65, wide"] = names()
+assert adapt([bank(cols=4096)], n=500, ids=None, y=[BASE], h=[H], room=1 << 30) == 0
 out["one adapter"] = names()
 assert grad(n=4, dx=BASE) == 0
 out["grad"] = names()
@@ -222,9 +226,9 @@ for n in (1, 31, 64, 65, 1000, 5000, 1 << 20):
             for ids in (0, 1):
                 assert need([bank(rank=rank, count=count)], n, ids)[0] == 0
 """]))
-    assert out["one token"] == ["expand"]
+    assert out["one token"] == out["64 of one adapter"] == ["expand"]
     assert out["a large first factor"] == out["64"] == out["one adapter"] == ["shrink", "expand"]
-    assert out["65"] == ["sort", "shrink", "expand"]
+    assert out["65"] == ["sort", "expand"] and out["65, wide"] == ["sort", "shrink", "expand"]
     assert out["grad"] == ["sort", "shrink", "expand", "outer"]
     assert out["grad of 300"] == ["sort", "shrink", "expand", "pack", "outer"]
     assert out["grad of many tokens"] == ["shrink", "expand", "pack", "outer", "outer_reduce"]
