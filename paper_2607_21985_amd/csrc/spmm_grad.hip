@@ -127,8 +127,8 @@ __global__ __launch_bounds__(kThreads) void grad_plain_kernel(GradArgs a) {
 // quarters, too. Values (per stripe one contiguous run) arrive by DMA in three
 // parts during the stripe before, a quarter's 64 rows of dY one quarter ahead,
 // 16-byte piece p of token t at place p ^ (t / 2 mod 8). The one barrier per
-// quarter stands in its last step, when all of the quarter's operands have been
-// read: what is requested behind it may overwrite them.
+// quarter stands where all of the quarter's operands have been read, two or four
+// MFMAs before its end: what is requested behind it may overwrite them.
 
 template <int TB, int CG, int TG>
 struct GradCfg {
@@ -291,10 +291,19 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
   load_rec1(r0, rec);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
   Walk k = walk(rec, r0, here);
-  issue_values(r0 + 1, 0, next);
+  // Values may be overwritten from the barrier on that follows the stripe's last
+  // read of them: its last one, or (32 tokens, whose barriers stand first in a
+  // quarter) the next stripe's first.
+  constexpr bool kEarly = TB == 1;
+  if (!kEarly) issue_values(r0 + 1, 0, next);
 
-  half8 x[2][TB];
-  Quad q[2];
+  // the tokens' operands are read kLead MFMAs ahead, the values kAhead steps
+  // (more for 64 tokens takes the registers of the second workgroup of a CU)
+  constexpr int kLead = TB == 2 ? 2 : 4;
+  constexpr int kSteps = TB == 1 ? 8 : 2;  // that x holds
+  constexpr int kAhead = TB == 1 ? 3 : 2;
+  half8 x[kSteps][TB];
+  Quad q[kAhead - 1][2];
   Window win;
   u32x2 first;  // the window's first word at the start of a stripe
   const uint32_t db = dyl + (uint32_t)(4096 * TB * tg) + 128u * (uint32_t)(lane & 31);
@@ -308,7 +317,7 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t b = w.mask[s >> 2] >> (8 * (s & 3) + 4 * i) & 15u;
-      q[i].read(w.p, lut + 8u * b);
+      q[s % (kAhead - 1)][i].read(w.p, lut + 8u * b);
       w.p += 2u * (uint32_t)__builtin_popcount(b);
     }
   };
@@ -316,31 +325,32 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
   auto build = [&](int s, int i) __attribute__((always_inline)) {
     if (s == 0 && i == 0) {
       win.a = first;
-      win.at = q[0].p & ~7u;
+      win.at = q[0][0].p & ~7u;
     }
-    w[i] = q[i].rows(win);
+    w[i] = q[s % (kAhead - 1)][i].rows(win);
   };
   read_q(k, 0);
   build(0, 0);
   build(0, 1);
-  read_q(k, 1);
-  // the tokens' operands are read kLead MFMAs ahead
-  constexpr int kLead = TB < 4 ? TB : 4;
 #pragma unroll
-  for (int t = 0; t < kLead; ++t) x[0][t] = read_x(0, 0, t);
+  for (int s = 1; s < kAhead; ++s) read_q(k, s);
+#pragma unroll
+  for (int e = 0; e < kLead; ++e) x[e / TB % kSteps][e % TB] = read_x(0, e / TB, e % TB);
 
   for (int r = r0; r < r1; ++r) {
     Run after;
     Walk kn;
 #pragma unroll
     for (int s = 0; s < 16; ++s) {
-      const int v = s >> 2, j = s & 3;
       if (s == 8) after = run_of(r + 2);
       const half8 now = __builtin_bit_cast(half8, u32x4{w[0][0], w[0][1], w[1][0], w[1][1]});
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < TB; ++t) {
-        if (j == 3 && t == TB - kLead) {
+        const int ahead = s * TB + t + kLead;
+        if (ahead % (4 * TB) == 0) {
+          // the operands of quarter v have all been read
+          const int v = ahead / (4 * TB) - 1;
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
           if (v == 2) {
             // the record is there: taken now, for the compiler's own wait for it
@@ -350,17 +360,19 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
           }
           if (v == 1) load_rec1(r + 1, rec);
           issue_dy(4 * r + v + 2, v & 1);
-          if (v == 3)
+          if (kEarly) {
+            if (v < 3) issue_values(r + 1, v, next);
+          } else if (v == 3) {
             issue_values(r + 2, 0, after);
-          else if (v < 2)
+          } else if (v < 2) {
             issue_values(r + 1, v + 1, next);
+          }
         }
-        const int ahead = s * TB + t + kLead;
-        x[ahead / TB & 1][ahead % TB] = read_x(ahead / TB >> 2, ahead / TB & 3, ahead % TB);
-        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[j & 1][t], now, acc[t], 0, 0, 0);
+        x[ahead / TB % kSteps][ahead % TB] = read_x(ahead / TB >> 2, ahead / TB & 3, ahead % TB);
+        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[s % kSteps][t], now, acc[t], 0, 0, 0);
         if (t == 0) build((s + 1) & 15, 0);
         if (t == (TB > 1 ? 1 : 0)) build((s + 1) & 15, 1);
-        if (t == (TB > 2 ? 2 : TB - 1)) read_q(s < 14 ? k : kn, (s + 2) & 15);
+        if (t == (TB > 2 ? 2 : TB - 1)) read_q(s + kAhead < 16 ? k : kn, (s + kAhead) & 15);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -416,10 +428,10 @@ struct Form {
   int lds(const spdp_matrix* h) const { return 2 * h->run_bytes[cg / 8] + 2 * tokens() * 128 + 256; }
 };
 constexpr Form kForms[] = {
-    {1, 4, 1, {0.66f, 0.80f, 1.23f, 1.37f}}, {2, 4, 1, {0.76f, 0.90f, 1.11f, 0.0f}},
-    {4, 4, 1, {0.95f, 1.18f, 0.0f, 0.0f}},   {4, 4, 2, {1.25f, 0.0f, 0.0f, 0.0f}},
-    {1, 8, 1, {0.80f, 1.10f, 0.0f, 0.0f}},   {2, 8, 1, {0.89f, 1.20f, 0.0f, 0.0f}},
-    {4, 8, 1, {1.11f, 0.0f, 0.0f, 0.0f}},    {8, 8, 1, {1.74f, 0.0f, 0.0f, 0.0f}}};
+    {1, 4, 1, {0.62f, 0.83f, 1.18f, 1.34f}}, {2, 4, 1, {0.75f, 0.90f, 1.14f, 0.0f}},
+    {4, 4, 1, {0.98f, 1.74f, 0.0f, 0.0f}},   {4, 4, 2, {1.27f, 0.0f, 0.0f, 0.0f}},
+    {1, 8, 1, {0.76f, 1.09f, 0.0f, 0.0f}},   {2, 8, 1, {0.90f, 1.22f, 0.0f, 0.0f}},
+    {4, 8, 1, {1.13f, 0.0f, 0.0f, 0.0f}},    {8, 8, 1, {1.75f, 0.0f, 0.0f, 0.0f}}};
 constexpr int kNumForms = sizeof(kForms) / sizeof(kForms[0]);
 
 struct GradPlan {
@@ -434,17 +446,18 @@ int env_int(const char* name, int otherwise) {
 }
 
 // us of a form with `splits` ranges of the stripes, by the model that the table
-// above is fitted to (1145 launches of 7 matrices at 16 to 2048 tokens, 7 % rms):
-// rounds of workgroups, 0.7 us each; 3 us and 8 bytes per sum at 5.6 TB/s for the
-// second launch that adds the ranges.
+// above is fitted to (1144 launches of 7 matrices at 16 to 2048 tokens, 8 % rms; the
+// choice loses 2.4 % on average to the best of all forms and splits): rounds of
+// workgroups, 1 us each; 1.9 us and 8 bytes per sum at 5.7 TB/s for the second
+// launch that adds the ranges.
 float model_us(const spdp_matrix* h, const Form& f, long long wgs, int per, int splits, long long n_tokens, int cus) {
   int most = 1;
   while (most < 4 && f.us[most] > 0.0f && (most + 1) * f.lds(h) <= kLdsMax) ++most;
   const long long full = wgs / ((long long)cus * most), rest = wgs - full * cus * most;
   const int k = (int)((rest + cus - 1) / cus);  // workgroups on a CU in the last round
   float us = (float)full * (4.0f * (float)per * f.us[most - 1] + 0.7f);
-  if (k > 0) us += 4.0f * (float)per * f.us[k - 1] + 0.7f;
-  if (splits > 1) us += 1.4f + (float)splits * (float)n_tokens * (float)h->cols * 8.0f / 5.6e6f;
+  if (k > 0) us += 4.0f * (float)per * f.us[k - 1] + 1.0f;
+  if (splits > 1) us += 1.9f + (float)splits * (float)n_tokens * (float)h->cols * 8.0f / 5.7e6f;
   return us;
 }
 
