@@ -50,16 +50,19 @@ struct HeadsArgs {
   int lanes;  // of a head: a power of two
 };
 
-// V fp16 as they are in memory
+// V fp16 as they are in memory (words of two, so that a pending load takes no more
+// registers than its bytes)
 template <int V>
 struct Raw {
-  uint16_t h[V];
-  __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(h, p, 2 * V); }
+  uint32_t w[(V + 1) / 2];
+  __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(w, p, 2 * V); }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int e = 0; e < V; ++e) h[e] = 0;
+    for (int e = 0; e < (V + 1) / 2; ++e) w[e] = 0;
   }
-  __device__ __forceinline__ float operator[](int e) const { return __half2float(__ushort_as_half(h[e])); }
+  __device__ __forceinline__ float operator[](int e) const {
+    return __half2float(__ushort_as_half((uint16_t)(w[e / 2] >> (e % 2 * 16))));
+  }
 };
 template <int V>
 __device__ __forceinline__ void store_v(uint16_t* p, const float (&v)[V]) {
@@ -93,13 +96,25 @@ struct Turn {
   __device__ __forceinline__ void load(const HeadsArgs& a, const Slot& t, long long pos, float sign) {
     const float* const tc = a.cosine + pos * a.half;
     const float* const ts = a.sine + pos * a.half;
+    const int at = PAIRS ? t.a / 2 : t.a;  // (b's angles follow a's)
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const int at = PAIRS ? t.a / 2 + e : t.a + e;  // (b's angles follow a's)
-      const bool in = t.turns && at < a.half;
-      c[e] = in ? tc[at] : 1.0f;
-      s[e] = in ? sign * ts[at] : 0.0f;
+      c[e] = 1.0f;
+      s[e] = 0.0f;
     }
+    if (t.turns && at + V <= a.half) {
+      __builtin_memcpy(c, tc + at, 4 * V);
+      __builtin_memcpy(s, ts + at, 4 * V);
+    } else if (PAIRS && at < a.half) {  // the leading numbers end within the vector
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (at + e < a.half) {
+          c[e] = tc[at + e];
+          s[e] = ts[at + e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] *= sign;
   }
   __device__ __forceinline__ void apply(float (&x)[2][V]) const {
 #pragma unroll
@@ -112,6 +127,23 @@ struct Turn {
     }
   }
 };
+
+// The sum over the 2^k lanes of a head, in each of them; all lanes are active. Lanes
+// that hold equal sums already may be met in any order, so that the mirrored rows
+// of the data-parallel moves will do.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float head_sum(float v, int lanes) {
+  if (lanes > 1) v += moved<0xb1>(v);    // 1 0 3 2
+  if (lanes > 2) v += moved<0x4e>(v);    // 2 3 0 1
+  if (lanes > 4) v += moved<0x141>(v);   // 8 lanes backwards
+  if (lanes > 8) v += moved<0x140>(v);   // 16 lanes backwards
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
+  return v;
+}
 
 // A workgroup of an input: its groups of lanes take `per` heads of a token
 // each, the groups of a wave all of one token.
@@ -136,13 +168,17 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   for (int r = 0; r < R; ++r) {
     t[r] = slot_of<V, PAIRS>(sub + 64 * r, a.half);
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
+      const int from = k == 0 ? t[r].a : t[r].b;
+      Raw<V> weights;
+      weights.clear();
+      if (norm && from < a.dim) weights.load(m.w + from);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const int at = (k == 0 ? t[r].a : t[r].b) + e;
-        w[r][k][e] = norm && at < a.dim ? __half2float(__ushort_as_half(m.w[at])) : 1.0f;
+        w[r][k][e] = norm ? weights[e] : 1.0f;
         dw[r][k][e] = 0.0f;
       }
+    }
   }
   const int wgs = (which + 1 < a.inputs ? a.m[which + 1].wg0 : (int)gridDim.x) - m.wg0;
   const long long rounds = (long long)a.n_tokens * chunks;
@@ -201,10 +237,8 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
           }
       }
       if (norm) {
-        for (int d = 1; d < a.lanes; d <<= 1) {
-          sum += __shfl_xor(sum, d);
-          if (BACK) dot += __shfl_xor(dot, d);
-        }
+        sum = head_sum(sum, a.lanes);
+        if (BACK) dot = head_sum(dot, a.lanes);
       }
       // (heads that are none, and padding, would divide by 0 where eps is 0)
       const float rms = norm && on && inside ? 1.0f / __fsqrt_rn(sum * inv_dim + a.eps) : 1.0f;
@@ -238,16 +272,22 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
     if (!norm) return;
     // the groups of a wave, then the waves in order
     __shared__ float red[kWaves][kMaxDim];
+    for (int d = a.lanes; d < 64; d <<= 1) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < V; ++e) dw[r][k][e] += __shfl_xor(dw[r][k][e], d);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          float v = dw[r][k][e];
-          for (int d = a.lanes; d < 64; d <<= 1) v += __shfl_xor(v, d);
           const int at = (k == 0 ? t[r].a : t[r].b) + e;
-          if (group == 0 && at < a.dim) red[wave][at] = v;
+          if (group == 0 && at < a.dim) red[wave][at] = dw[r][k][e];
         }
     __syncthreads();
     for (int i = threadIdx.x; i < a.dim; i += kThreads)
@@ -324,8 +364,9 @@ void plan_heads(const spdp_heads_t* in, int inputs, const spdp_rotation_t* r, lo
     sum += rounds[i];
   }
   // backward: each workgroup's share of the weights' gradient is reduced, written
-  // and read again: as many as a CU's registers hold (2048 tokens, 40 + 8 heads of
-  // 96, with 1 / 2 / 3 / 4 per CU: 43 / 34 / 29 / 34 us)
+  // and read again: as many as a CU's registers hold (2 / 3 / 4 per CU: 2048
+  // tokens, 40 + 8 heads of 96, 26 / 21 / 23 us; 512, 64 + 8 of 128, 15 / 14 / 18;
+  // 4096, 32 + 8 of 128, 35 / 31 / 29)
   const long long most = back ? 3ll * cus : 1ll << 22;
   p->wg0[0] = 0;
   for (int i = 0; i < inputs; ++i) {
