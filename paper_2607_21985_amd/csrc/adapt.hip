@@ -269,6 +269,7 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
   const int first = (int)blockIdx.x * kBlock + wave * kCols + 8 * (lane & 7);
   const int stride = (int)gridDim.x * kBlock;
   const uint16_t* const factor = m.factor + (size_t)max(adapter, 0) * a.rank * m.width;
+  const float scale = m.scale[max(adapter, 0)];
   size_t row[kPasses];  // of the lane's tokens
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) row[p] = (size_t)tok[8 * p + (lane >> 3)] * m.width;
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
   const bool lead = blockIdx.x == 0;
   const int t = threadIdx.x >> 3;
   if (t < T) {
-    const size_t at0 = (size_t)tok[t] * a.rank;
+    const uint32_t at0 = (uint32_t)tok[t] * (uint32_t)a.rank;  // (2^20 tokens, 128 ranks at most)
     if (adapter >= 0) {
       const size_t plane = (size_t)a.t.n_tokens * a.rank;
       float v[2 * RB];
@@ -323,20 +324,19 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
         for (int i = 0; i < 2 * RB; ++i)  // (ranks that are none repeat the last)
           if (8 * i + part8 >= a.rank) v[i] = 0.0f;
       } else {
-        // all ranks of four ranges in flight, added in order
-        for (int s0 = 0; s0 < m.splits; s0 += 4) {
-          float x[4][2 * RB];
+        // all ranks of some ranges in flight, added in order
+        constexpr int S = RB <= 2 ? 4 : 2;
+        for (int s0 = 0; s0 < m.splits; s0 += S) {
+          float x[S][2 * RB];
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
+          for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int i = 0; i < 2 * RB; ++i) {
-              const int j = 8 * i + part8;
-              x[s][i] = s0 + s < m.splits && j < a.rank ? m.part[(s0 + s) * plane + at0 + j] : 0.0f;
-            }
+            for (int i = 0; i < 2 * RB; ++i)
+              x[s][i] = (m.part + min(s0 + s, m.splits - 1) * plane)[at0 + (uint32_t)min(8 * i + part8, a.rank - 1)];
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
+          for (int s = 0; s < S; ++s)
 #pragma unroll
-            for (int i = 0; i < 2 * RB; ++i) v[i] += x[s][i];
+            for (int i = 0; i < 2 * RB; ++i) v[i] += s0 + s < m.splits && 8 * i + part8 < a.rank ? x[s][i] : 0.0f;
         }
       }
 #pragma unroll
@@ -358,12 +358,13 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
         *reinterpret_cast<_Float16*>(act_lo + at) = lo;
       }
       if (part8 == 0) {
-        mult[t] = down * m.scale[adapter];
+        mult[t] = down * scale;
         if (m.most != nullptr && lead && t < count) m.most[tok[t]] = largest;
       }
       if (m.most != nullptr && lead && t < count) {
         float other = 0.0f;
-        for (int j = part8; j < a.rank; j += 8) other = fmaxf(other, finite_abs(m.other[at0 + j]));
+#pragma unroll
+        for (int i = 0; i < 2 * RB; ++i) other = fmaxf(other, finite_abs(m.other[at0 + (uint32_t)min(8 * i + part8, a.rank - 1)]));
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) other = fmaxf(other, __shfl_xor(other, d));
         if (part8 == 0) m.most[a.t.n_tokens + tok[t]] = other;
@@ -488,6 +489,17 @@ __device__ __forceinline__ void piece_scale(const OuterArgs& a, const Outer& m, 
   pick_scale(largest, up, down);
 }
 
+// The places of the tokens t .. t + 7 of a piece that ends at t1; those past its
+// end repeat its last (loads without a branch each are in flight together).
+__device__ __forceinline__ void rows_of(const OuterArgs& a, int t, int t1, int (&at)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) at[e] = min(t + e, t1 - 1);
+  if (a.perm) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) at[e] = a.perm[at[e]];
+  }
+}
+
 template <int RB>  // 32 RB ranks
 __global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
   __shared__ float all[kWaves];
@@ -503,12 +515,17 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
   for (int q = (int)blockIdx.x * kThreads + threadIdx.x; q < groups * RB * 64; q += (int)gridDim.x * kThreads) {
     const int lane = q & 63, block = (q >> 6) % RB, g = (q >> 6) / RB;
     const int j = 32 * block + (lane & 31);
+    const int t = p.t0 + g * kGroup + 8 * (lane >> 5);
+    int at[8];
+    float v[8];
     half8 hi, lo;
+    rows_of(a, t, p.t1, at);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = m.act[(uint32_t)at[e] * (uint32_t)a.rank + (uint32_t)min(j, a.rank - 1)];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int t = p.t0 + g * kGroup + 8 * (lane >> 5) + e;
       _Float16 h, l;
-      split2(t < p.t1 && j < a.rank ? m.act[(size_t)(a.perm ? a.perm[t] : t) * a.rank + j] * up : 0.0f, h, l);
+      split2(t + e < p.t1 && j < a.rank ? v[e] * up : 0.0f, h, l);
       hi[e] = h;
       lo[e] = l;
     }
@@ -567,16 +584,12 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
       if (at[p] >= 0 && left > 0) in[p] = load8_inside(m.in + (size_t)at[p] * m.width + col, left);
     }
     if constexpr (DIRECT) {
+      int from[8];
+      rows_of(a, piece.t0 + g * kGroup + 8 * (lane >> 5), piece.t1, from);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = piece.t0 + g * kGroup + 8 * (lane >> 5) + e;
-        const float* const p = m.act + (size_t)(t < piece.t1 ? (a.perm ? a.perm[t] : t) : 0) * a.rank;
+      for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int j = 0; j < RB; ++j) {
-          raw[j][e] = 0.0f;
-          if (t < piece.t1 && 32 * j + (lane & 31) < a.rank) raw[j][e] = p[32 * j + (lane & 31)];
-        }
-      }
+        for (int j = 0; j < RB; ++j) raw[j][e] = m.act[(uint32_t)from[e] * (uint32_t)a.rank + (uint32_t)min(32 * j + (lane & 31), a.rank - 1)];
     } else {
 #pragma unroll
       for (int j = 0; j < 2 * RB; ++j) act[j] = packed[(size_t)g * RB * 128 + 64 * j];
@@ -599,7 +612,8 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           _Float16 hi, lo;
-          split2(raw[j][e] * up, hi, lo);
+          const bool there = piece.t0 + g * kGroup + 8 * (lane >> 5) + e < piece.t1 && 32 * j + (lane & 31) < a.rank;
+          split2(there ? raw[j][e] * up : 0.0f, hi, lo);
           now[2 * j][e] = hi;
           now[2 * j + 1][e] = lo;
         }
@@ -1077,9 +1091,9 @@ void plan_grad(const spdp_adapters_t* m, long long n_tokens, bool ids, int cus, 
   const size_t each = (size_t)p->splits * m->count * m->rank * 4;
   p->outer[0] = p->splits > 1 ? aligned(each * m->cols) : 0;
   p->outer[1] = p->splits > 1 ? aligned(each * m->rows) : 0;
-  // (backward passes of rank 16, 4096 x 4096, packed / direct: 32 tokens 18.3 / 16.3
-  // us, 256 of two adapters 26.8 / 25.0, 512 22.5 / 24.2)
-  const bool packed = n_tokens > 256;
+  // (backward passes, 4096 x 4096, packed / direct: 200 tokens of rank 16 16.8 / 15.0
+  // us, 400 of four adapters 24.9 / 22.8, 800 of eight of rank 64 41.0 / 42.9)
+  const bool packed = n_tokens > 512;
   p->packed = packed ? packed_bytes(m, n_tokens, p->splits) : 0;
   p->down = packed ? aligned((size_t)m->count * p->splits * 4) : 0;
   p->most = aligned((size_t)n_tokens * 8);
