@@ -79,6 +79,10 @@ SIZES = [
     (200, 512, 1024, 2, 128, "runs"),
     (1025, 128, 136, 2048, 2, "mixed"),
     (2100, 72, 520, 3, 100, "runs"),
+    (512, 96, 1032, 5, 70, "mixed"),
+    (513, 520, 96, 1, 24, "none"),
+    (600, 200, 152, 3, 40, "mixed"),
+    (700, 1000, 1000, 1, 128, "same"),
 ]
 
 
