@@ -79,8 +79,8 @@ __device__ __forceinline__ bool take_tile(const Tokens& t, int block, int* tok, 
 }
 
 // ---------------------------------------------------------------------------
-// Shrink. A workgroup owns a tile of tokens and a range of the width, its four
-// waves every fourth step of 64 columns; 16x16x32 MFMAs with the tokens as
+// Shrink. A workgroup owns a tile of tokens and a range of the width, its four (or
+// eight) waves every fourth (eighth) step of 64 columns; 16x16x32 MFMAs with the tokens as
 // rows. The waves' sums are added in LDS.
 
 constexpr int kStep = 64;
@@ -176,8 +176,8 @@ __device__ __forceinline__ void shrink_steps(const uint16_t* in, const uint16_t*
         red[((wave * T + 16 * i + 4 * (lane >> 4) + e) * RB + j) * 16 + (lane & 15)] = acc[i][j][e];
 }
 
-template <int RB, int T>  // 16 RB ranks, tiles of T tokens
-__global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
+template <int RB, int T, int W>  // 16 RB ranks, tiles of T tokens, W waves
+__global__ __launch_bounds__(64 * W) void shrink_kernel(ShrinkArgs a) {
   __shared__ int tok[T];
   extern __shared__ __attribute__((aligned(16))) float red[];  // [wave][token][16 RB]
   const Shrink& m = a.m[blockIdx.z];
@@ -186,16 +186,16 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(ShrinkArgs a) {
   const int steps = (m.width + kStep - 1) / kStep;
   const int s0 = (int)blockIdx.y * m.per;
   if (s0 >= steps) return;  // the grid has the most ranges of the launch's products
-  shrink_steps<RB, T, kWaves>(m.in, m.factor + (size_t)adapter * a.rank * m.width, m.width, a.rank, tok, s0,
+  shrink_steps<RB, T, W>(m.in, m.factor + (size_t)adapter * a.rank * m.width, m.width, a.rank, tok, s0,
                               min(steps, s0 + m.per), red);
   __syncthreads();
   float* const part = m.part + (size_t)blockIdx.y * a.t.n_tokens * a.rank;
-  for (int q = threadIdx.x; q < count * 16 * RB; q += kThreads) {
+  for (int q = threadIdx.x; q < count * 16 * RB; q += 64 * W) {
     const int t = q / (16 * RB), j = q % (16 * RB);
     if (j >= a.rank) continue;
     float sum = red[q];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) sum += red[w * T * 16 * RB + q];
+    for (int w = 1; w < W; ++w) sum += red[w * T * 16 * RB + q];
     part[(size_t)tok[t] * a.rank + j] = sum;
   }
 }
@@ -933,13 +933,18 @@ int sort_tokens(const int32_t* ids, long long n, int count, const SortPlan& p, u
 
 template <int RB, int T>
 hipError_t launch_shrink_form(const ShrinkArgs& a, dim3 grid, hipStream_t st) {
-  const int lds = kWaves * T * 16 * RB * 4;
+  // eight waves where a wave's registers let two of them share a SIMD and it loads
+  // one step at a time (2048 tokens, rank 32, 28672 wide: the backward pass 133 ->
+  // 116 us); smaller forms load two steps at a time and would wait longer for their
+  // sums (32 tokens, rank 16, 4096 x 4096: 8.4 -> 9.4)
+  constexpr int W = RB + T / 16 == 6 ? 2 * kWaves : kWaves;
+  const int lds = W * T * 16 * RB * 4;
   if (lds > kLdsPlain) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(shrink_kernel<RB, T>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(shrink_kernel<RB, T, W>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((shrink_kernel<RB, T>), grid, dim3(kThreads), lds, st, a);
+  hipLaunchKernelGGL((shrink_kernel<RB, T, W>), grid, dim3(64 * W), lds, st, a);
   return hipGetLastError();
 }
 template <int RB>
