@@ -325,7 +325,7 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
           if (8 * i + part8 >= a.rank) v[i] = 0.0f;
       } else {
         // all ranks of some ranges in flight, added in order
-        constexpr int S = RB <= 2 ? 4 : 2;
+        constexpr int S = RB >= 4 ? 2 : 8 / RB;
         for (int s0 = 0; s0 < m.splits; s0 += S) {
           float x[S][2 * RB];
 #pragma unroll
