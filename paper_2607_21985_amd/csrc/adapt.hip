@@ -22,6 +22,13 @@
 // power of two, so that the largest lies in [2^13, 2^14), and split into the
 // nearest fp16 and the rest's nearest fp16: 22 bits or, for small ones, 2^-38
 // of the largest. Two MFMAs instead of one; the launches are bound by memory.
+//
+// Measured, on a card that copies at 5.2 TB/s: shrink_kernel, 2048 tokens, 8192
+// wide, rank 32, 11.6 us (34 MB of input, 2.9 TB/s, and the factor from L2);
+// expand_kernel behind it, 28672 wide, 55 us (235 MB, 4.3 TB/s); outer_kernel, 4096
+// tokens, 13824 + 5120 wide, rank 64, 45 us (155 MB, 3.4 TB/s); sort_kernel, 2048
+// ids, 6 us, a chain of LDS round trips. Small calls are bound by the launches,
+// 4 to 7 us each.
 
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -428,8 +435,8 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = (_Float16)__fmaf_rn(by, sum[e], (float)mybase[p][e]);
       }
-      // (an output that the L2 caches cannot hold does not go through them: 2048
-      // tokens, 28672 wide, 71.5 -> 69 us, 4096 x 4096 28.5 -> 24.5)
+      // (an output that the L2 caches cannot hold does not go through them: the
+      // whole pass over 2048 tokens, 28672 wide, 80.4 -> 77.8 us)
       if (m.stream && left >= 8) {
         typedef half8 half8_any __attribute__((aligned(2)));
         __builtin_nontemporal_store(y, reinterpret_cast<half8_any*>(m.out + row[p] + col));
@@ -811,9 +818,9 @@ int compute_units(int* cus) {
 
 // The ranges of the width that shrink_kernel's workgroups take: one workgroup
 // per CU, at least four steps each (one per wave), at most eight ranges, for
-// expand_kernel's workgroups all add them (4096 tokens of rank 64, 13824 wide,
-// with 2 / 4 / 8 / 16 ranges: 53 / 32 / 33 / 37 us; 4096 wide behind 1000
-// tokens the other product takes 10 us with 4 ranges and 15 with 16).
+// expand_kernel's workgroups all add them (whole passes of rank 64 with 2 / 4 / 8 /
+// 16 ranges: 4096 tokens, 13824 to 5120, 89 / 66 / 70 / 83 us; 1000, 11008 to 4096, 40 /
+// 27 / 22 / 26).
 struct Ranges {
   int per, splits;
 };
@@ -829,15 +836,15 @@ Ranges shrink_ranges(int64_t width, long long tiles, int banks, int cus) {
 // tokens are split into, and the waves of a workgroup: pieces of many tokens, four
 // workgroups per CU (of three that a CU holds); unsplit, eight waves where there
 // are fewer than two workgroups per CU. Whole backward passes, us, unsplit of
-// four waves / of eight / split: 4096 tokens, 13824 x 5120, rank 64 150 / 154 /
-// 134; 2048, 4096 x 11008, rank 16 64 / 55 / 57; 4000 of 8 adapters, 8192 x 8192,
-// rank 8 106 / 109 / 118.
+// four waves / of eight / split: 4096 tokens, 13824 x 5120, rank 64 143 / 144 /
+// 129; 2048, 4096 x 11008, rank 16 62 / 53 / 54; 4000 of 8 adapters, 8192 x 8192,
+// rank 8 107 / 111 / 108.
 //
 // Much input and ranks up to 64: 128 columns, which read the packed activations
 // half as often (they come from L2, twice the input's bytes at rank 64 and 64
 // columns), and the pieces that fill the two workgroups that a CU holds best
-// (4096 tokens, 13824 x 5120, rank 64 132 -> 124 us; 16384, 4096 x 4096, rank 16
-// 169 -> 158; 3000, 11008 x 4096, rank 32 would take 79 for 76).
+// (4096 tokens, 13824 x 5120, rank 64 129 -> 120 us; 16384, 4096 x 4096, rank 16
+// 167 -> 155; 3000, 11008 x 4096, rank 32 would take 77 for 74).
 long long outer_wgs(const spdp_adapters_t* m, int cols) {
   return ((m->rows + cols - 1) / cols + (m->cols + cols - 1) / cols) * m->count;
 }
@@ -981,7 +988,7 @@ hipError_t launch_fused_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_t
   return tile == 16 ? launch_expand_form<RB, 16, true>(a, grid, st) : launch_expand_form<RB, 32, true>(a, grid, st);
 }
 hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused, int cus, hipStream_t st) {
-  // (with 64 tokens a workgroup of expand_kernel is slower: 65 us for 56 of 2048
+  // (with 64 tokens a workgroup of expand_kernel was slower: 65 us for 56 of 2048
   // tokens of rank 32, 28672 wide, 33 for 30 of 4096 of rank 64, 5120 wide)
   a.subs = p.tile > 32 ? p.tile / 32 : 1;
   const long long tiles = p.tiles * a.subs;
@@ -990,9 +997,8 @@ hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused
   const int block = kCols * (fused ? kFusedWaves : kWaves);
   const int blocks = (widest + block - 1) / block;
   // a workgroup keeps its tokens' activations for several blocks where that
-  // leaves the three workgroups that a CU holds (2048 tokens of rank 32, 28672
-  // wide, with 2 / 3 / 5 / 8 blocks: 70 / 67 / 61 / 72 us; 4096 of rank 64, 5120
-  // wide, with 2 / 4 / 8: 37 / 34 / 35)
+  // leaves the three workgroups that a CU holds (whole passes over 2048 tokens of
+  // rank 32, 28672 wide, with 2 / 3 / 5 / 8 blocks: 79 / 80 / 78 / 90 us)
   const long long fill = (fused ? 1ll : 3ll) * cus;
   a.blocks = (int)std::max<long long>(1, std::min<long long>(5, (blocks * tiles * banks + fill - 1) / fill));
   const dim3 grid((unsigned)((blocks + a.blocks - 1) / a.blocks), (unsigned)tiles, (unsigned)banks);
@@ -1062,11 +1068,10 @@ void plan_adapt(const spdp_adapters_t* banks, int n_banks, long long n_tokens, b
   p->splits = 1;
   // The fused form, where a workgroup's own pass over the first factor (at 16,
   // 32 or 64 ranks) is short and the workgroups that make it are few. Two
-  // launches -> fused, us per pass, called in sequence and from a graph: one
-  // token of rank 8, 1024 wide, 11.4 / 7.0 -> 8.7 / 5.1; 24 of 5 adapters of rank
-  // 12, 5003 x 3080, 10.9 / 8.4 -> 8.2 / 8.1; one of rank 16, 4096 wide, 10.9 / 7.6
-  // -> 9.0 / 8.8; 333 of 4 adapters of rank 16, 1024 wide (and the sort) 13.9 /
-  // 13.5 -> 12.2 / 12.1, 4096 wide 15.1 / 14.2 -> 20.8 / 20.9.
+  // launches -> fused, us per pass from a graph: one token of rank 8, 1024 wide, 6.5
+  // -> 4.5; 24 of 5 adapters of rank 12, 5003 x 3080, 7.6 -> 7.7, a launch less for
+  // the host; one of rank 16, 4096 wide, 6.2 -> 8.2; 333 of 4 adapters of rank 16,
+  // 1024 wide (and the sort) 13.4 -> 11.8, 4096 wide 14.2 -> 21.2.
   long long wgs = 0;
   p->fused = p->sort.tile <= 32 && banks[0].rank <= 64;
   for (int i = 0; i < n_banks; ++i) {
