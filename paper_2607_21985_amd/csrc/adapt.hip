@@ -1020,7 +1020,7 @@ hipError_t launch_outer_form(const OuterArgs& a, int widest, hipStream_t st) {
     if constexpr (RB <= 2 && !DIRECT) hipLaunchKernelGGL((outer_kernel<RB, 4, 4, false>), grid, dim3(256), 0, st, a);
   } else if (a.waves == 4) {
     hipLaunchKernelGGL((outer_kernel<RB, 4, 2, DIRECT>), grid, dim3(256), 0, st, a);
-  } else {
+  } else if constexpr (!DIRECT || RB <= 2) {
     hipLaunchKernelGGL((outer_kernel<RB, 8, 2, DIRECT>), grid, dim3(512), 0, st, a);
   }
   return hipGetLastError();
@@ -1272,7 +1272,9 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   oa.splits = p.splits;
   oa.wide = outer_wide(bank, n_tokens);
   oa.packed = p.packed > 0;
-  oa.waves = !split && outer_wgs(bank, kCols) < 2 * cus ? 8 : 4;
+  // (the direct form of more than 64 ranks spills registers with eight: 39.3 us of 64
+  // tokens of four adapters, rank 128, 4096 x 4096, with either)
+  oa.waves = !split && outer_wgs(bank, kCols) < 2 * cus && (oa.packed || bank->rank <= 64) ? 8 : 4;
   e = launch_outer(oa, (int)std::max(bank->rows, bank->cols), s);
   if (e == hipSuccess && split) {
     ReduceArgs ra;

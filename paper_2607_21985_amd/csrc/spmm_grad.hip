@@ -229,7 +229,7 @@ __global__ __launch_bounds__(64 * CG * TG) void grad_kernel(GradArgs a) {
     if (r >= r1 || u.t1 <= u.t0) return;
     const uint32_t last = u.t1 - u.t0 - 16u;
     const uint32_t to = val + (uint32_t)(r & 1) * (uint32_t)a.run;
-    for (uint32_t at = 1024u * (uint32_t)(W * q + wave); at <= last; at += 3072u * W)
+    for (uint32_t at = 1024u * (uint32_t)(W * q + wave); at <= last; at += 3u * 1024u * W)
       dma16(a.values, u.t0 + min(at + 16u * (uint32_t)lane, last),
             (uint32_t)__builtin_amdgcn_readfirstlane((int)(to + at)));
   };

@@ -207,8 +207,8 @@ assert adapt([bank(cols=4096)], n=500, ids=None, y=[BASE], h=[H], room=1 << 30) 
 out["one adapter"] = names()
 assert grad(n=4, dx=BASE) == 0
 out["grad"] = names()
-assert grad(n=300) == 0
-out["grad of 300"] = names()
+assert grad(n=600) == 0
+out["grad of 600"] = names()
 assert grad(bank(count=1), n=4096, ids=None) == 0
 out["grad of many tokens"] = names()
 assert rotate([one(y=X), one(x=Y, y=Y + (1 << 30))]) == 0
@@ -230,7 +230,7 @@ for n in (1, 31, 64, 65, 1000, 5000, 1 << 20):
     assert out["a large first factor"] == out["64"] == out["one adapter"] == ["shrink", "expand"]
     assert out["65"] == ["sort", "expand"] and out["65, wide"] == ["sort", "shrink", "expand"]
     assert out["grad"] == ["sort", "shrink", "expand", "outer"]
-    assert out["grad of 300"] == ["sort", "shrink", "expand", "pack", "outer"]
+    assert out["grad of 600"] == ["sort", "shrink", "expand", "pack", "outer"]
     assert out["grad of many tokens"] == ["shrink", "expand", "pack", "outer", "outer_reduce"]
     assert out["heads"] == out["heads grad without weights"] == ["heads"]
     assert out["heads grad"] == ["heads", "heads_sum"]
