@@ -254,7 +254,7 @@ struct ExpandCfg {
   static_assert(W != kFusedWaves || T * kRank * 4 <= kWave, "the waves' shares of h fit");
 };
 
-template <int RB, int T, bool FUSED>  // 16 RB ranks, tiles of T <= 32 tokens
+template <int RB, int T, bool FUSED, bool ONCE>  // 16 RB ranks, tiles of T <= 32 tokens; ONCE: past the caches
 __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_kernel(ExpandArgs a) {
   constexpr int W = FUSED ? kFusedWaves : kWaves;
   constexpr int kBlock = kCols * W;
@@ -290,7 +290,8 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
     if (left <= 0) return;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p)
-      if (part == 0 && 8 * p + (lane >> 3) < count) base[p] = load8_inside(m.base + row[p] + col, left);
+      if (part == 0 && 8 * p + (lane >> 3) < count)
+        base[p] = ONCE ? load8_once(m.base + row[p] + col, left) : load8_inside(m.base + row[p] + col, left);
     if (adapter < 0) return;
 #pragma unroll
     for (int p = 0; p < 2 * C::kPart; ++p) {
@@ -435,9 +436,11 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = (_Float16)__fmaf_rn(by, sum[e], (float)mybase[p][e]);
       }
-      // (an output that the L2 caches cannot hold does not go through them: the
-      // whole pass over 2048 tokens, 28672 wide, 80.4 -> 77.8 us)
-      if (m.stream && left >= 8) {
+      // (an output that the L2 caches cannot hold does not go through them, nor does
+      // its base: whole passes, through them / the output past them / both, 2048 tokens,
+      // 28672 wide, 80.4 / 77.8 / 75.5 us, 4000 tokens of 8 adapters, 8192 wide, the
+      // latter two 66.7 / 60.8)
+      if (ONCE && left >= 8) {
         typedef half8 half8_any __attribute__((aligned(2)));
         __builtin_nontemporal_store(y, reinterpret_cast<half8_any*>(m.out + row[p] + col));
       } else {
@@ -586,9 +589,15 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
   };
   auto request = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < FB; ++p) {
-      in[p] = none;
-      if (at[p] >= 0 && left > 0) in[p] = load8_inside(m.in + (size_t)at[p] * m.width + col, left);
+    for (int p = 0; p < FB; ++p) in[p] = none;
+    if (!DIRECT && m.stream) {
+#pragma unroll
+      for (int p = 0; p < FB; ++p)
+        if (at[p] >= 0 && left > 0) in[p] = load8_once(m.in + (size_t)at[p] * m.width + col, left);
+    } else {
+#pragma unroll
+      for (int p = 0; p < FB; ++p)
+        if (at[p] >= 0 && left > 0) in[p] = load8_inside(m.in + (size_t)at[p] * m.width + col, left);
     }
     if constexpr (DIRECT) {
       int from[8];
@@ -967,25 +976,33 @@ hipError_t launch_shrink(const ShrinkArgs& a, int tile, dim3 grid, hipStream_t s
   return launch_shrink_rb<8>(a, tile, grid, st);
 }
 
-template <int RB, int T, bool FUSED>
+// Outputs, or an input, of all tokens that are larger than the L2 caches (4 MB on
+// each of 8 dies). The outer products' inputs go past the caches, too, for nothing
+// reads them afterwards: backward passes of 4096 tokens, rank 64, 13824 x 5120,
+// 118.6 -> 112.3 us; 1000 of rank 64, 4096 x 11008, which fit, would take 43.1 for 41.
+bool streams(long long n_tokens, int64_t width) { return n_tokens * width * 2 > 32ll << 20; }
+
+template <int RB, int T, bool FUSED, bool ONCE>
 hipError_t launch_expand_form(const ExpandArgs& a, dim3 grid, hipStream_t st) {
   constexpr int W = FUSED ? kFusedWaves : kWaves;
   const int lds = ExpandCfg<RB, T, W>::kLds;
   if (lds > kLdsPlain) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(expand_kernel<RB, T, FUSED>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(expand_kernel<RB, T, FUSED, ONCE>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((expand_kernel<RB, T, FUSED>), grid, dim3(64 * W), lds, st, a);
+  hipLaunchKernelGGL((expand_kernel<RB, T, FUSED, ONCE>), grid, dim3(64 * W), lds, st, a);
   return hipGetLastError();
 }
 template <int RB>
-hipError_t launch_expand_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_t st) {
-  return tile == 16 ? launch_expand_form<RB, 16, false>(a, grid, st) : launch_expand_form<RB, 32, false>(a, grid, st);
+hipError_t launch_expand_rb(const ExpandArgs& a, int tile, bool once, dim3 grid, hipStream_t st) {
+  if (once)
+    return tile == 16 ? launch_expand_form<RB, 16, false, true>(a, grid, st) : launch_expand_form<RB, 32, false, true>(a, grid, st);
+  return tile == 16 ? launch_expand_form<RB, 16, false, false>(a, grid, st) : launch_expand_form<RB, 32, false, false>(a, grid, st);
 }
 template <int RB>
 hipError_t launch_fused_rb(const ExpandArgs& a, int tile, dim3 grid, hipStream_t st) {
-  return tile == 16 ? launch_expand_form<RB, 16, true>(a, grid, st) : launch_expand_form<RB, 32, true>(a, grid, st);
+  return tile == 16 ? launch_expand_form<RB, 16, true, false>(a, grid, st) : launch_expand_form<RB, 32, true, false>(a, grid, st);
 }
 hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused, int cus, hipStream_t st) {
   // (with 64 tokens a workgroup of expand_kernel was slower: 65 us for 56 of 2048
@@ -993,7 +1010,11 @@ hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused
   a.subs = p.tile > 32 ? p.tile / 32 : 1;
   const long long tiles = p.tiles * a.subs;
   int widest = 0;
-  for (int i = 0; i < banks; ++i) widest = std::max(widest, a.m[i].width);
+  int64_t all = 0;
+  for (int i = 0; i < banks; ++i) {
+    widest = std::max(widest, a.m[i].width);
+    all += a.m[i].width;
+  }
   const int block = kCols * (fused ? kFusedWaves : kWaves);
   const int blocks = (widest + block - 1) / block;
   // a workgroup keeps its tokens' activations for several blocks where that
@@ -1002,14 +1023,16 @@ hipError_t launch_expand(ExpandArgs& a, int banks, const SortPlan& p, bool fused
   const long long fill = (fused ? 1ll : 3ll) * cus;
   a.blocks = (int)std::max<long long>(1, std::min<long long>(5, (blocks * tiles * banks + fill - 1) / fill));
   const dim3 grid((unsigned)((blocks + a.blocks - 1) / a.blocks), (unsigned)tiles, (unsigned)banks);
+  // (the fused form's outputs are never so large)
+  const bool once = streams(a.t.n_tokens, all);
   if (fused)
     return a.rank <= 16   ? launch_fused_rb<1>(a, p.tile, grid, st)
            : a.rank <= 32 ? launch_fused_rb<2>(a, p.tile, grid, st)
                           : launch_fused_rb<4>(a, p.tile, grid, st);
-  if (a.rank <= 16) return launch_expand_rb<1>(a, p.tile, grid, st);
-  if (a.rank <= 32) return launch_expand_rb<2>(a, p.tile, grid, st);
-  if (a.rank <= 64) return launch_expand_rb<4>(a, p.tile, grid, st);
-  return launch_expand_rb<8>(a, p.tile, grid, st);
+  if (a.rank <= 16) return launch_expand_rb<1>(a, p.tile, once, grid, st);
+  if (a.rank <= 32) return launch_expand_rb<2>(a, p.tile, once, grid, st);
+  if (a.rank <= 64) return launch_expand_rb<4>(a, p.tile, once, grid, st);
+  return launch_expand_rb<8>(a, p.tile, once, grid, st);
 }
 
 template <int RB, bool DIRECT>
@@ -1110,9 +1133,6 @@ void plan_grad(const spdp_adapters_t* m, long long n_tokens, bool ids, int cus, 
   p->bytes = p->sort.bytes + p->part + p->u + p->outer[0] + p->outer[1] + 2 * (p->packed + p->down) + p->most;
 }
 
-// an output larger than the L2 caches (4 MB on each of 8 dies)
-int streams(long long n_tokens, int64_t width) { return n_tokens * width * 2 > 32ll << 20; }
-
 int check_workspace(const void* workspace, size_t have, size_t need) {
   if (need == 0) return SPDP_OK;
   if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
@@ -1183,7 +1203,7 @@ int adapt(const spdp_adapters_t* banks, int32_t n_banks, const uint16_t* const* 
     if (!p.fused) ws += part_bytes(n_tokens, b.rank, p.r[i].splits);
     sa.m[i] = Shrink{X[i], b.a, part, (int)b.cols, p.r[i].per};
     ea.m[i] = Expand{part, b.b, b.scale, base[i], Y[i], H ? H[i] : nullptr, nullptr, nullptr, X[i], b.a,
-                       (int)b.rows, p.fused ? 1 : p.r[i].splits, (int)b.cols, streams(n_tokens, b.rows)};
+                       (int)b.rows, p.fused ? 1 : p.r[i].splits, (int)b.cols};
   }
   hipError_t e = hipSuccess;
   if (!p.fused) e = launch_shrink(sa, p.sort.tile, dim3((unsigned)p.sort.tiles, (unsigned)p.splits, (unsigned)n_banks), s);
@@ -1255,15 +1275,14 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   sa.t = ea.t = t;
   sa.rank = ea.rank = oa.rank = bank->rank;
   sa.m[0] = Shrink{dY, bank->b, part, (int)bank->rows, p.r.per};
-  ea.m[0] = Expand{part, bank->a, bank->scale, base, dX, u, most, H, nullptr, nullptr, (int)bank->cols, p.r.splits, 0,
-                   streams(n_tokens, bank->cols)};
+  ea.m[0] = Expand{part, bank->a, bank->scale, base, dX, u, most, H, nullptr, nullptr, (int)bank->cols, p.r.splits, 0};
   hipError_t e = launch_shrink(sa, p.sort.tile, dim3((unsigned)p.sort.tiles, (unsigned)p.r.splits, 1), s);
   if (e == hipSuccess) e = launch_expand(ea, 1, p.sort, false, cus, s);
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   const bool split = p.splits > 1;
-  oa.m[0] = Outer{u, X, split ? pa : dA, most, packed, down, (int)bank->cols};
+  oa.m[0] = Outer{u, X, split ? pa : dA, most, packed, down, (int)bank->cols, streams(n_tokens, bank->cols)};
   oa.m[1] = Outer{H, dY, split ? pb : dB, most + n_tokens, packed + p.packed,
-                  down + p.down / 4, (int)bank->rows};
+                  down + p.down / 4, (int)bank->rows, streams(n_tokens, bank->rows)};
   oa.scale = bank->scale;
   oa.perm = t.perm;
   oa.first = first;

@@ -39,6 +39,12 @@ __device__ __forceinline__ void store8_inside(uint16_t* p, half8 v, int n) {
 }
 __device__ __forceinline__ half8 load8_inside(const uint16_t* p, int n) { return n >= 8 ? load8(p) : load_upto8(p, n); }
 
+// the same of data that is larger than the caches and read once
+__device__ __forceinline__ half8 load8_once(const uint16_t* p, int n) {
+  typedef half8 half8_any __attribute__((aligned(2)));
+  return n >= 8 ? __builtin_nontemporal_load(reinterpret_cast<const half8_any*>(p)) : load_upto8(p, n);
+}
+
 // lane's operand of the 32 columns from `col` on and the eight rows from `row`
 // + 8 (lane / 32) on, of a row-major fp16 tile in LDS of `stride` bytes a row.
 // Each group of 16 lanes reads 4 rows x 16 columns: lane i supplies the address

@@ -62,7 +62,6 @@ struct Expand {
   int width;
   int splits;
   int in_width;
-  int stream;  // the output is larger than the caches
 };
 struct ExpandArgs {
   Expand m[kMaxBanks];
@@ -82,6 +81,7 @@ struct Outer {
   unsigned char* packed; // the activations as operands
   float* down;           // [adapter][split]: what their scale has to be undone with
   int width;
+  int stream;            // the input is larger than the caches
 };
 struct OuterArgs {
   Outer m[2];
