@@ -52,12 +52,23 @@ struct HeadsArgs {
   int lanes;  // of a head: a power of two
 };
 
+// 16 bytes at any address of fp16
+typedef uint32_t Vec __attribute__((ext_vector_type(4), aligned(2)));
+
 // V fp16 as they are in memory (words of two, so that a pending load takes no more
 // registers than its bytes)
 template <int V>
 struct Raw {
   uint32_t w[(V + 1) / 2];
-  __device__ __forceinline__ void load(const uint16_t* p) { __builtin_memcpy(w, p, 2 * V); }
+  template <bool ONCE>
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    if constexpr (ONCE) {
+      const Vec v = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(p));
+      __builtin_memcpy(w, &v, 2 * V);
+    } else {
+      __builtin_memcpy(w, p, 2 * V);
+    }
+  }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int e = 0; e < (V + 1) / 2; ++e) w[e] = 0;
@@ -66,12 +77,18 @@ struct Raw {
     return __half2float(__ushort_as_half((uint16_t)(w[e / 2] >> (e % 2 * 16))));
   }
 };
-template <int V>
+template <int V, bool ONCE>
 __device__ __forceinline__ void store_v(uint16_t* p, const float (&v)[V]) {
   uint16_t h[V];
 #pragma unroll
   for (int e = 0; e < V; ++e) h[e] = __half_as_ushort(__float2half_rn(v[e]));
-  __builtin_memcpy(p, h, 2 * V);
+  if constexpr (ONCE) {
+    Vec v;
+    __builtin_memcpy(&v, h, 2 * V);
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec*>(p));
+  } else {
+    __builtin_memcpy(p, h, 2 * V);
+  }
 }
 
 // A lane's place in a head: the vectors at a and b (past the end: none), and
@@ -148,8 +165,9 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 }
 
 // A workgroup of an input: its groups of lanes take `per` heads of a token
-// each, the groups of a wave all of one token.
-template <int V, int R, bool PAIRS, bool BACK>
+// each, the groups of a wave all of one token. ONCE: outputs (backward: inputs,
+// too) go past the caches, which cannot hold them.
+template <int V, int R, bool PAIRS, bool BACK, bool ONCE>
 __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
   int which = 0;
   while (which + 1 < a.inputs && (int)blockIdx.x >= a.m[which + 1].wg0) ++which;
@@ -174,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
       const int from = k == 0 ? t[r].a : t[r].b;
       Raw<V> weights;
       weights.clear();
-      if (norm && from < a.dim) weights.load(m.w + from);
+      if (norm && from < a.dim) weights.template load<false>(m.w + from);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         w[r][k][e] = norm ? weights[e] : 1.0f;
@@ -205,8 +223,8 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
           nx[r][k].clear();
           if (BACK) ng[r][k].clear();
           if (h < m.heads && inside && from < a.dim) {
-            if (!BACK || norm) nx[r][k].load(m.x + at + from);
-            if (BACK) ng[r][k].load(m.dy + at + from);
+            if (!BACK || norm) nx[r][k].template load<ONCE && BACK>(m.x + at + from);
+            if (BACK) ng[r][k].template load<ONCE>(m.dy + at + from);
           }
         }
     };
@@ -264,8 +282,8 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
           }
         if (!BACK) u[r].apply(o);
         if (on) {
-          if (t[r].a < a.dim) store_v<V>(m.y + at + t[r].a, o[0]);
-          if (t[r].b < a.dim) store_v<V>(m.y + at + t[r].b, o[1]);
+          if (t[r].a < a.dim) store_v<V, ONCE>(m.y + at + t[r].a, o[0]);
+          if (t[r].b < a.dim) store_v<V, ONCE>(m.y + at + t[r].b, o[1]);
         }
       }
     }
@@ -397,18 +415,18 @@ int check(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
   return SPDP_OK;
 }
 
-template <int V, int R, bool PAIRS>
+template <int V, int R, bool PAIRS, bool ONCE>
 void launch(const HeadsArgs& a, bool back, dim3 grid, hipStream_t s) {
   if (back)
-    hipLaunchKernelGGL((heads_kernel<V, R, PAIRS, true>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((heads_kernel<V, R, PAIRS, true, ONCE>), grid, dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((heads_kernel<V, R, PAIRS, false>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((heads_kernel<V, R, PAIRS, false, ONCE>), grid, dim3(kThreads), 0, s, a);
 }
-template <int V, int R>
+template <int V, int R, bool ONCE>
 void launch_pairs(const HeadsArgs& a, bool pairs, bool back, dim3 grid, hipStream_t s) {
   if constexpr (V > 1)
-    if (pairs) return launch<V, R, true>(a, back, grid, s);
-  launch<V, R, false>(a, back, grid, s);
+    if (pairs) return launch<V, R, true, ONCE>(a, back, grid, s);
+  launch<V, R, false, ONCE>(a, back, grid, s);
 }
 
 int compute_units(int* cus) {
@@ -489,7 +507,9 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
     }
   }
   unsigned char* ws = static_cast<unsigned char*>(workspace);
+  size_t bytes = 0;
   for (int i = 0; i < inputs; ++i) {
+    bytes += (size_t)n_tokens * in[i].heads * r->dim * 2;
     a.m[i] = HeadsInput{in[i].x, in[i].weight, in[i].dy, in[i].y, nullptr, in[i].heads, p.wg0[i], p.per[i]};
     if (back && in[i].weight) {
       const int wgs = p.wg0[i + 1] - p.wg0[i];
@@ -513,14 +533,21 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
   a.lanes = p.lanes;
   const dim3 grid((unsigned)p.wg0[inputs]);
   auto s = static_cast<hipStream_t>(stream);
-  if (p.v == 8)
-    launch_pairs<8, 1>(a, pairs, back, grid, s);
+  // Outputs larger than the L2 caches (4 MB on each of 8 dies) go past them, and the
+  // backward pass's inputs, which nothing reads afterwards (through / past them:
+  // 4096 tokens of 32 + 32 heads of 128 31.3 / 24.8 us, backward 51.6 / 46.4; 2048 of
+  // 40 + 8 of 96, which fit, 10.3 / 13.2, 20.3 / 22.2)
+  const bool once = bytes > (size_t)32 << 20;
+  if (p.v == 8 && once)
+    launch_pairs<8, 1, true>(a, pairs, back, grid, s);
+  else if (p.v == 8)
+    launch_pairs<8, 1, false>(a, pairs, back, grid, s);
   else if (p.v == 2 && p.rounds == 1)
-    launch_pairs<2, 1>(a, pairs, back, grid, s);
+    launch_pairs<2, 1, false>(a, pairs, back, grid, s);
   else if (p.v == 2)
-    launch_pairs<2, 2>(a, pairs, back, grid, s);
+    launch_pairs<2, 2, false>(a, pairs, back, grid, s);
   else
-    launch_pairs<1, 4>(a, pairs, back, grid, s);
+    launch_pairs<1, 4, false>(a, pairs, back, grid, s);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && sums > 0) {
     hipLaunchKernelGGL(heads_sum_kernel, dim3((unsigned)((r->dim + 15) / 16), (unsigned)sums), dim3(1024), 0, s, sum);
