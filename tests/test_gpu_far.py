@@ -120,6 +120,40 @@ def test_heads_beyond_32_bits():
     assert torch.isfinite(dw).all()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_heads_larger_than_the_caches(interleaved):
+    # two inputs of rows one number into their memory, with padding, a part of
+    # the head rotated; in place gives the same bits
+    n, dim, rot, counts = 9001, 112, 96, (20, 3)
+    shift = lambda v: torch.cat([torch.zeros(1, dtype=torch.float16, device="cuda"), v.reshape(-1)])[1:].view(v.shape)  # noqa: E731
+    xs = [shift(_filled(n, k * dim)) for k in counts]
+    dys = [shift(_filled(n, k * dim, 0.1)) for k in counts]
+    rng = np.random.default_rng(4)
+    pos = rng.integers(-1, 301, n).astype(np.int32)
+    ang = np.arange(300)[:, None] * np.exp(-np.log(1e4) * np.arange(0, rot, 2) / rot)
+    cos, sin = np.cos(ang).astype(np.float32), np.sin(ang).astype(np.float32)
+    w = (1 + 0.1 * rng.normal(size=dim)).astype(np.float16)
+    tabs, ws = (_dev(pos), _dev(cos), _dev(sin)), [_dev(w), None]
+    ys = [shift(torch.full_like(x, 7.0)) for x in xs]
+    spdp.rotate_heads(xs, dim, *tabs, ys, weights=ws, interleaved=interleaved)
+    dxs, dw = [shift(torch.zeros_like(x)) for x in xs], [torch.empty(dim, device="cuda"), None]
+    spdp.rotate_heads_grad(xs, dim, *tabs, dys, dxs, weights=ws, dweights=dw, interleaved=interleaved)
+    at = _rows(n)
+    sel = torch.from_numpy(at).cuda()
+    for x, dy, y, dx, weight in zip(xs, dys, ys, dxs, (w, None)):
+        xh, was = _np(x[sel]), np.full((len(at), x.shape[1]), 7.0)
+        want, bound = layer.heads(xh, dim, pos[at], cos, sin, weight, 1e-6, interleaved, was)
+        assert np.all(np.abs(_np(y[sel]) - want) <= bound)
+        (want, bound), _ = layer.heads_grad(xh, dim, pos[at], cos, sin, _np(dy[sel]), weight, 1e-6, interleaved)
+        assert np.all(np.abs(_np(dx[sel]) - want) <= bound)
+    inside = torch.from_numpy((pos >= 0) & (pos < 300)).cuda()
+    again, dw2 = [v.clone() for v in dys], [torch.empty_like(dw[0]), None]
+    spdp.rotate_heads_grad(xs, dim, *tabs, again, again, weights=ws, dweights=dw2, interleaved=interleaved)
+    assert torch.equal(again[0], dxs[0]) and torch.equal(again[1], dxs[1]) and torch.equal(dw[0], dw2[0])
+    spdp.rotate_heads(xs, dim, *tabs, xs, weights=ws, interleaved=interleaved)
+    assert all(torch.equal(x[inside], y[inside]) for x, y in zip(xs, ys))
+
+
 def test_pruned_gradient_beyond_32_bits():
     rows, cols, n = 32_776, 72, 66_000
     assert n * rows > 1 << 31
