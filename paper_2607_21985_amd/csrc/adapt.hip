@@ -24,9 +24,9 @@
 // of the largest. Two MFMAs instead of one; the launches are bound by memory.
 //
 // Measured, on a card that copies at 5.2 TB/s: shrink_kernel, 2048 tokens, 8192
-// wide, rank 32, 11.6 us (34 MB of input, 2.9 TB/s, and the factor from L2);
-// expand_kernel behind it, 28672 wide, 55 us (235 MB, 4.3 TB/s); outer_kernel, 4096
-// tokens, 13824 + 5120 wide, rank 64, 45 us (155 MB, 3.4 TB/s); sort_kernel, 2048
+// wide, rank 32, 11.2 us (34 MB of input, 3 TB/s, and the factor from L2);
+// expand_kernel behind it, 28672 wide, 54 us (235 MB, 4.4 TB/s); outer_kernel, 4096
+// tokens, 13824 + 5120 wide, rank 64, 42 us (155 MB, 3.7 TB/s); sort_kernel, 2048
 // ids, 6 us, a chain of LDS round trips. Small calls are bound by the launches,
 // 4 to 7 us each.
 
