@@ -495,7 +495,8 @@ class Adapters:
     ``a`` is fp16 [count, rank, cols], ``b`` fp16 [count, rank, rows] (the
     second factor rank by rank), ``scale`` fp32 [count], all contiguous on one
     GPU. Nothing is copied: weights that are changed in place, or replaced by
-    others of the same shape, count from the next call on.
+    others of the same shape, count from the next call on. Every call looks at
+    the weights anew, and refuses those of another shape, type or layout.
 
         y = fp16(base + scale[id] * (x a[id]^T) b[id])
 
@@ -504,26 +505,35 @@ class Adapters:
     """
 
     def __init__(self, a, b, scale):
+        import torch
         if a.dim() != 3 or b.dim() != 3:
             raise ValueError("a and b must be [count, rank, features]")
         self.a, self.b, self.scale = a, b, scale
         self.count, self.rank, self.cols = a.shape
         self.rows = b.shape[2]
+        self._form = (torch.float16, torch.float32, a.shape, torch.Size((self.count, self.rank, self.rows)),
+                      torch.Size((self.count,)))
+        self._key = (self.rows, self.cols, self.rank, self.count)
         self._pointers = None
         self._sizes = {}  # workspaces of calls, by their sizes
         need = ctypes.c_size_t()  # checks the sizes
         _check(lib().spdp_adapt_workspace(self._struct(), 1, 1, 0, ctypes.byref(need)))
 
     def _struct(self) -> bytes:
-        # the tensors may have been given other memory (``p.data = ...``) or
-        # replaced since the last call
-        at = (self.a.data_ptr(), self.b.data_ptr(), self.scale.data_ptr())
+        # the tensors may have been replaced since the last call, or given other
+        # memory (``p.data = ...``), by ones of another shape, type or layout, too,
+        # and at the same address: a view of the old ones, or what the allocator
+        # has put in their place
+        a, b, scale = self.a, self.b, self.scale
+        half, single, of_a, of_b, of_scale = self._form
+        if not (a.dtype is half and b.dtype is half and scale.dtype is single and a.shape == of_a and b.shape == of_b
+                and scale.shape == of_scale and a.is_contiguous() and b.is_contiguous() and scale.is_contiguous()):
+            _tensor(a, "a", half, of_a)
+            _tensor(b, "b", half, of_b)
+            _tensor(scale, "scale", single, of_scale)
+        at = (a.data_ptr(), b.data_ptr(), scale.data_ptr())
         if at != self._pointers:
-            import torch
-            _tensor(self.a, "a", torch.float16, (self.count, self.rank, self.cols))
-            _tensor(self.b, "b", torch.float16, (self.count, self.rank, self.rows))
-            _tensor(self.scale, "scale", torch.float32, (self.count,))
-            _stream(None, (self.a, self.b, self.scale))
+            _stream(None, (a, b, scale))
             self._bank = _PACK_BANK.pack(*at, self.rows, self.cols, self.count, self.rank)
             self._pointers = at
         return self._bank
@@ -557,8 +567,8 @@ class Adapters:
         _tensor(dy, "dy", torch.float16, (n, self.rows))
         _tensor(base, "base", torch.float16, (n, self.cols))
         _tensor(dx, "dx", torch.float16, (n, self.cols))
-        _tensor(da, "da", torch.float32, self.a.shape)
-        _tensor(db, "db", torch.float32, self.b.shape)
+        _tensor(da, "da", torch.float32, self._form[2])
+        _tensor(db, "db", torch.float32, self._form[3])
         some = (x, h, dy, base, dx, da, db, self.a)
         if ids is not None:
             _tensor(ids, "ids", torch.int32, (n,))
@@ -587,7 +597,7 @@ def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
     for m, x, base, y in zip(banks, xs, bases, ys):
         bk.append(m._struct())
         some.append(m.a)
-        key += (m.rows, m.cols, m.rank, m.count)
+        key.append(m._key)
         _tensor(x, "x", f16, (n, m.cols))
         out = (n, m.rows)
         _tensor(base, "base", f16, out)

@@ -1,0 +1,108 @@
+"""The binding of the adapters', heads' and gradient calls, without a GPU: which
+tensors reach the library (its entry points are recorded, and tensors of host
+memory pass for a GPU's)."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2607_21985_amd as spdp  # noqa: E402
+
+
+class _Library:
+    """Records the calls; each succeeds."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append(name)
+            return 0
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    rec = _Library()
+    monkeypatch.setattr(spdp, "lib", lambda: rec)
+    monkeypatch.setattr(spdp, "_stream", lambda stream, tensors: 0)
+    return rec
+
+
+def _half(*shape):
+    return torch.zeros(shape, dtype=torch.float16)
+
+
+COUNT, RANK, COLS, ROWS, TOKENS = 4, 8, 8, 24, 5
+
+
+def _calls(bank):
+    """Every call that reads the bank's weights."""
+    x, base, ids = _half(TOKENS, COLS), _half(TOKENS, ROWS), torch.zeros(TOKENS, dtype=torch.int32)
+    h = torch.zeros(TOKENS, RANK)
+    da, db = torch.zeros(COUNT, RANK, COLS), torch.zeros(COUNT, RANK, ROWS)
+    yield lambda: bank.add_into(x, ids, base, torch.empty_like(base))
+    yield lambda: bank(x, ids, base)
+    yield lambda: spdp.adapters_many([bank], [x], None, [base], [torch.empty_like(base)], hs=[h])
+    yield lambda: bank.grad_into(x, ids, h, base, x, torch.empty_like(x), da, db)
+
+
+# replacements at the address of the weights that they replace
+SAME_ADDRESS = {
+    "fewer adapters": (lambda b: ("a", b.a[:2]), ValueError),
+    "fewer ranks": (lambda b: ("a", b.a[:, :4]), ValueError),
+    "fewer rows": (lambda b: ("b", b.b[:, :, :8]), ValueError),
+    "fewer scales": (lambda b: ("scale", b.scale[:3]), ValueError),
+    "another order": (lambda b: ("a", b.a.transpose(1, 2)), ValueError),  # (as many ranks as columns)
+    "broadcast scales": (lambda b: ("scale", b.scale[:1].expand(COUNT)), ValueError),
+    "another type": (lambda b: ("a", b.a.view(torch.bfloat16)), TypeError),
+    "whole numbers": (lambda b: ("scale", b.scale.view(torch.int32)), TypeError),
+}
+
+
+@pytest.mark.parametrize("how", SAME_ADDRESS)
+def test_replaced_weights_are_looked_at(library, how):
+    change, error = SAME_ADDRESS[how]
+    for k in range(4):
+        bank = spdp.Adapters(_half(COUNT, RANK, COLS), _half(COUNT, RANK, ROWS), torch.zeros(COUNT))
+        call = list(_calls(bank))[k]
+        call()
+        name, new = change(bank)
+        assert new.data_ptr() == getattr(bank, name).data_ptr()
+        setattr(bank, name, new)
+        library.calls.clear()
+        with pytest.raises(error):
+            call()
+        assert not library.calls
+
+
+def test_weights_whose_memory_is_replaced_are_looked_at(library):
+    bank = spdp.Adapters(_half(COUNT, RANK, COLS), _half(COUNT, RANK, ROWS), torch.zeros(COUNT))
+    bank.b.data = bank.b.data[:1]
+    for call in _calls(bank):
+        library.calls.clear()
+        with pytest.raises(ValueError):
+            call()
+        assert not library.calls
+
+
+def test_gradients_have_the_banks_own_shapes(library):
+    # the shapes that the kernels write, whatever the weights' are by now
+    bank = spdp.Adapters(_half(COUNT, RANK, COLS), _half(COUNT, RANK, ROWS), torch.zeros(COUNT))
+    x, dy, h = _half(TOKENS, COLS), _half(TOKENS, ROWS), torch.zeros(TOKENS, RANK)
+    bank.a = bank.a[:2]
+    library.calls.clear()
+    with pytest.raises(ValueError, match="da"):
+        bank.grad_into(x, None, h, dy, x, torch.empty_like(x), torch.zeros(2, RANK, COLS), torch.zeros(COUNT, RANK, ROWS))
+    assert not library.calls
+
+
+def test_weights_of_the_same_form_may_be_replaced(library):
+    bank = spdp.Adapters(_half(COUNT, RANK, COLS), _half(COUNT, RANK, ROWS), torch.zeros(COUNT))
+    bank.a, bank.scale = bank.a.clone(), bank.scale + 1
+    bank.b.data = bank.b.data.clone()
+    for call in _calls(bank):
+        library.calls.clear()
+        call()
+        assert library.calls
