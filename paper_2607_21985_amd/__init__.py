@@ -763,17 +763,23 @@ class Chain:
     product as a plain call. ``add_adapters`` and ``add_heads`` record what
     stands between them: the requests' adapters, and the norm and rotation of
     the heads. ``capture`` sizes every matrix's workspace for
-    the batches recorded, issues the launches once eagerly and records them
-    into a graph on a side stream; ``replay`` re-issues the whole chain on
+    the batches recorded, issues the launches once eagerly (what works in place
+    changes its tensors then, too) and records them into a graph on a side stream; ``replay`` re-issues the whole chain on
     the current stream with one host call. Between replays the caller
     rewrites the input tensors in place (and the thresholds are fixed at
     capture); the calls keep no host-side state, so every replay computes on
-    the tensors' current contents.
+    the tensors' current contents, those of the adapters' and heads' weights,
+    too. The graph has the addresses that the weights had at capture: where one
+    has been replaced since (another tensor, or ``p.data = ...``), ``replay``
+    raises, and the chain has to be captured again.
     """
 
     def __init__(self):
         self._calls = []
         self._graph = None
+        self._weights = []   # of the recorded calls: Adapters, and the heads' tensors
+        self._captured = []  # where the graph reads them
+        self._alive = ()     # and that memory, which a replaced tensor would give back
 
     def add(self, mats, xs, thresholds, ys, mask: str = "token") -> "Chain":
         if self._graph is not None:
@@ -791,6 +797,7 @@ class Chain:
         if isinstance(banks, Adapters):
             banks, xs, bases, ys = [banks], [xs], [bases], [ys]
         args = (list(banks), list(xs), ids, list(bases), list(ys))
+        self._weights += args[0]
         self._calls.append((None, args[1], None, lambda: adapters_many(*args), None))
         return self
 
@@ -799,6 +806,7 @@ class Chain:
         if self._graph is not None:
             raise RuntimeError("the chain is captured already")
         args = (list(xs), dim, pos, cos, sin, list(ys), None if weights is None else list(weights), eps, interleaved)
+        self._weights += [w for w in weights or [] if w is not None]
         self._calls.append((None, args[0], None, lambda: rotate_heads(*args), None))
         return self
 
@@ -810,6 +818,9 @@ class Chain:
                 mats[0].spmspv_into(xs[0], ts[0], ys[0], mask=mask)
             else:
                 spmspv_many(mats, xs, ts, ys, mask=mask)
+
+    def _addresses(self) -> list:
+        return [w._struct() if isinstance(w, Adapters) else w.data_ptr() for w in self._weights]
 
     def capture(self) -> "Chain":
         import torch
@@ -827,10 +838,15 @@ class Chain:
         with torch.cuda.graph(g, stream=s):
             self._issue()
         torch.cuda.current_stream(dev).wait_stream(s)
+        self._captured = self._addresses()
+        self._alive = [t.detach() for w in self._weights
+                       for t in ((w.a, w.b, w.scale) if isinstance(w, Adapters) else (w,))]
         self._graph = g
         return self
 
     def replay(self) -> None:
         if self._graph is None:
             raise RuntimeError("capture() first")
+        if self._weights and self._addresses() != self._captured:
+            raise RuntimeError("weights of adapters or heads were replaced since capture(): capture the chain again")
         self._graph.replay()

@@ -106,3 +106,88 @@ def test_weights_of_the_same_form_may_be_replaced(library):
         library.calls.clear()
         call()
         assert library.calls
+
+
+class _Graph:
+    replays = 0
+
+    def replay(self):
+        _Graph.replays += 1
+
+
+@pytest.fixture
+def graphs(library, monkeypatch):
+    """torch's streams and graphs stand still; the chain's own calls are recorded."""
+    import contextlib
+
+    class Stream:
+        def __init__(self, device=None):
+            pass
+
+        def wait_stream(self, other):
+            pass
+
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: Stream())
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda dev=None: None)
+    monkeypatch.setattr(torch.cuda, "CUDAGraph", _Graph)
+    monkeypatch.setattr(torch.cuda, "graph", lambda g, stream=None: contextlib.nullcontext())
+    _Graph.replays = 0
+    return library
+
+
+def _chain():
+    bank = spdp.Adapters(_half(COUNT, RANK, COLS), _half(COUNT, RANK, ROWS), torch.zeros(COUNT))
+    weight, tables = _half(8), (torch.zeros(TOKENS, dtype=torch.int32), torch.zeros(9, 4), torch.zeros(9, 4))
+    y = _half(TOKENS, ROWS)
+    ch = spdp.Chain().add_adapters(bank, _half(TOKENS, COLS), None, y, y)
+    return ch.add_heads([y], 8, *tables, [y], weights=[weight]), bank, weight
+
+
+def _new_data(t):
+    t.data = t.data.clone()
+
+
+REPLACED = {
+    "a": lambda bank, weight: setattr(bank, "a", bank.a.clone()),
+    "b's memory": lambda bank, weight: _new_data(bank.b),
+    "scale": lambda bank, weight: setattr(bank, "scale", bank.scale * 2),
+    "the norm's memory": lambda bank, weight: _new_data(weight),
+}
+
+
+@pytest.mark.parametrize("what", REPLACED)
+def test_a_chain_notices_replaced_weights(graphs, what):
+    ch, bank, weight = _chain()
+    ch.capture()
+    ch.replay()
+    old = [t.data_ptr() for t in (bank.a, bank.b, bank.scale, weight)]
+    REPLACED[what](bank, weight)
+    for _ in range(2):
+        with pytest.raises(RuntimeError, match="captur"):
+            ch.replay()
+    assert _Graph.replays == 1
+    # the captured memory is not handed out again while the graph is there
+    assert [t.data_ptr() for t in ch._alive] == old
+    ch.capture()
+    ch.replay()
+    assert _Graph.replays == 2
+
+
+def test_a_chain_replays_weights_rewritten_in_place(graphs):
+    ch, bank, weight = _chain()
+    ch.capture()
+    bank.a += 1
+    bank.scale.mul_(2)
+    weight += 1
+    ch.replay()
+    assert _Graph.replays == 1
+
+
+def test_a_chain_refuses_weights_of_another_form(graphs):
+    ch, bank, _ = _chain()
+    ch.capture()
+    bank.a = bank.a[:2]  # at the same address
+    with pytest.raises(ValueError):
+        ch.replay()
+    assert _Graph.replays == 0
