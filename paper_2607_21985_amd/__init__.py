@@ -238,6 +238,20 @@ def _workspace(size: int, device, stream):
         return torch.empty(size or 1, dtype=torch.uint8, device=device)
 
 
+def _output(shape, device, stream):
+    """An fp16 array that a call writes and the caller gets. It is taken, like a
+    workspace, as the call's stream's own (what else is queued on the caller's
+    may still use a block of that one's), and kept from reuse until what the
+    caller's stream does with it is done, too."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=torch.float16, device=device)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=torch.float16, device=device)
+    out.record_stream(torch.cuda.current_stream(device))
+    return out
+
+
 class Matrix:
     """An encoded weight matrix (owns the library handle)."""
 
@@ -381,9 +395,8 @@ class Matrix:
         _check(lib().spdp_spmm_grad(self._h, dy.data_ptr(), n, dx.data_ptr(), ws.data_ptr(), need.value, s))
 
     def spmm_grad(self, dy, stream=None):
-        """The gradient ``dy W_sp`` as a new fp16 tensor."""
-        import torch
-        dx = torch.empty((dy.shape[0], self.cols), dtype=torch.float16, device=dy.device)
+        """The gradient ``dy W_sp`` as a new fp16 tensor (which belongs to ``stream``)."""
+        dx = _output((dy.shape[0], self.cols), dy.device, stream)
         self.spmm_grad_into(dy, dx, stream)
         return dx
 
@@ -548,9 +561,8 @@ class Adapters:
         adapters_many([self], [x], ids, [base], [y], None if h is None else [h], stream)
 
     def __call__(self, x, ids, base, stream=None):
-        """``add_into`` a new tensor."""
-        import torch
-        y = torch.empty_like(base)
+        """``add_into`` a new tensor (which belongs to ``stream``)."""
+        y = _output(base.shape, base.device, stream)
         self.add_into(x, ids, base, y, stream=stream)
         return y
 

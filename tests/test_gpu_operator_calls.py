@@ -69,3 +69,29 @@ def test_a_chain_whose_weights_change():
         ch.capture()
         check()
         assert not torch.equal(z, before)
+
+
+def test_results_on_another_stream():
+    # the current stream has work left on a block that it has given back: a result
+    # on another stream must not take it
+    torch.manual_seed(2)
+    n, rows, cols = 200, 512, 512
+    bank = _bank(2, 16, rows, cols)
+    w = np.random.default_rng(3).normal(size=(rows, cols)).astype(np.float16)
+    w[np.random.default_rng(4).random(w.shape) < 0.5] = 0
+    m = spdp.encode(w, (256, 16))
+    x, base = _half(n, cols), _half(n, rows)
+    ids = torch.randint(-1, 2, (n,), device="cuda", dtype=torch.int32)
+    side = torch.cuda.Stream()
+    for call in (lambda s: bank(x, ids, base, stream=s), lambda s: m.spmm_grad(base, stream=s)):
+        want = call(None)
+        torch.cuda.synchronize()
+        scratch = torch.empty_like(want)
+        torch.cuda._sleep(20_000_000)
+        scratch.fill_(float("nan"))
+        del scratch
+        got = call(side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+    m.close()

@@ -191,3 +191,56 @@ def test_a_chain_refuses_weights_of_another_form(graphs):
     with pytest.raises(ValueError):
         ch.replay()
     assert _Graph.replays == 0
+
+
+@pytest.fixture
+def streams(library, monkeypatch):
+    """Which stream each tensor was taken on, by address, and the streams that
+    were recorded for it; "caller" is the current one."""
+    import contextlib
+    state = {"current": "caller", "taken": {}, "recorded": {}}
+
+    @contextlib.contextmanager
+    def on(stream):
+        state["current"], before = stream, state["current"]
+        yield
+        state["current"] = before
+
+    empty, empty_like = torch.empty, torch.empty_like
+
+    def taken(t):
+        state["taken"][t.data_ptr()] = state["current"]
+        return t
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: state["current"])
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: taken(empty(*a, **k)))
+    monkeypatch.setattr(torch, "empty_like", lambda *a, **k: taken(empty_like(*a, **k)))
+    monkeypatch.setattr(torch.Tensor, "record_stream",
+                        lambda t, s: state["recorded"].setdefault(t.data_ptr(), []).append(s))
+    return state
+
+
+def _matrix():
+    m = spdp.Matrix.__new__(spdp.Matrix)
+    m._h, m.rows, m.cols, m.device = None, ROWS, COLS, 0
+    return m
+
+
+VALUES = {
+    "adapters": lambda bank, m, s: bank(_half(TOKENS, COLS), None, _half(TOKENS, ROWS), stream=s),
+    "pruned gradient": lambda bank, m, s: m.spmm_grad(_half(TOKENS, ROWS), stream=s),
+}
+
+
+@pytest.mark.parametrize("what", VALUES)
+def test_results_belong_to_the_calls_stream(streams, what):
+    bank = spdp.Adapters(_half(COUNT, RANK, COLS), _half(COUNT, RANK, ROWS), torch.zeros(COUNT))
+    m = _matrix()
+    out = VALUES[what](bank, m, "side")
+    assert out.dtype == torch.float16 and tuple(out.shape) == (TOKENS, COLS if what == "pruned gradient" else ROWS)
+    assert streams["taken"][out.data_ptr()] == "side"
+    assert streams["recorded"][out.data_ptr()] == ["caller"]
+    streams["recorded"].clear()
+    out = VALUES[what](bank, m, None)
+    assert streams["taken"][out.data_ptr()] == "caller" and not streams["recorded"]
