@@ -375,9 +375,8 @@ class Matrix:
                                ctypes.c_void_p(s.cuda_stream)))
 
     def spmm(self, x, stream=None):
-        """The prefill product ``x W_sp^T`` as a new fp16 tensor."""
-        import torch
-        y = torch.empty((x.shape[0], self.rows), dtype=torch.float16, device=x.device)
+        """The prefill product ``x W_sp^T`` as a new fp16 tensor (which belongs to ``stream``)."""
+        y = _output((x.shape[0], self.rows), x.device, stream)
         self.spmm_into(x, y, stream)
         return y
 
@@ -401,8 +400,7 @@ class Matrix:
         return dx
 
     def __call__(self, x, threshold: float, stream=None, mask: str = "token"):
-        import torch
-        y = torch.empty((x.shape[0], self.rows), dtype=torch.float16, device=x.device)
+        y = _output((x.shape[0], self.rows), x.device, stream)
         self.spmspv_into(x, threshold, y, stream, mask)
         return y
 

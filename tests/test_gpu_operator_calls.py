@@ -83,7 +83,8 @@ def test_results_on_another_stream():
     x, base = _half(n, cols), _half(n, rows)
     ids = torch.randint(-1, 2, (n,), device="cuda", dtype=torch.int32)
     side = torch.cuda.Stream()
-    for call in (lambda s: bank(x, ids, base, stream=s), lambda s: m.spmm_grad(base, stream=s)):
+    for call in (lambda s: bank(x, ids, base, stream=s), lambda s: m.spmm_grad(base, stream=s),
+                 lambda s: m.spmm(x, stream=s), lambda s: m(x[:4], 0.1, stream=s)):
         want = call(None)
         torch.cuda.synchronize()
         scratch = torch.empty_like(want)

@@ -244,3 +244,15 @@ def test_results_belong_to_the_calls_stream(streams, what):
     streams["recorded"].clear()
     out = VALUES[what](bank, m, None)
     assert streams["taken"][out.data_ptr()] == "caller" and not streams["recorded"]
+
+
+@pytest.mark.parametrize("call", [lambda m, s: m.spmm(_half(TOKENS, COLS), stream=s),
+                                  lambda m, s: m(_half(TOKENS, COLS), 0.5, stream=s)])
+def test_products_belong_to_the_calls_stream(streams, monkeypatch, call):
+    into = []
+    monkeypatch.setattr(spdp.Matrix, "spmm_into", lambda self, x, y, stream=None: into.append((y, stream)))
+    monkeypatch.setattr(spdp.Matrix, "spmspv_into", lambda self, x, t, y, stream=None, mask="token": into.append((y, stream)))
+    out = call(_matrix(), "side")
+    assert into == [(out, "side")] and tuple(out.shape) == (TOKENS, ROWS)
+    assert streams["taken"][out.data_ptr()] == "side" and streams["recorded"][out.data_ptr()] == ["caller"]
+    assert streams["taken"][call(_matrix(), None).data_ptr()] == "caller"
