@@ -316,7 +316,8 @@ typedef struct spdp_adapters {
  *   X, base, Y n_banks device pointers each (X[i]: n_tokens x cols_i, base[i]
  *              and Y[i]: n_tokens x rows_i, fp16, row-major). Any alignment
  *              that fp16 has. X may be shared. Y[i] may be base[i]; else an
- *              output overlaps no input and no other output.
+ *              output (H among them) overlaps no input, the banks' arrays and
+ *              ids included, and no other output.
  *   ids        device, n_tokens; an id outside [0, count) is no adapter, and
  *              the token's Y is its base. NULL: adapter 0 for every token.
  *   H          NULL, or n_banks device pointers (n_tokens x rank fp32 each)
@@ -355,7 +356,8 @@ int spdp_adapt(const spdp_adapters_t* banks, int32_t n_banks,
  *   dY         device, n_tokens x rows fp16.
  *   base, dX   device, n_tokens x cols fp16; dX may be base.
  *   dA, dB     device, fp32, laid out as a and b, fully overwritten (adapters
- *              without tokens: 0).
+ *              without tokens: 0). Else no output overlaps an input or another
+ *              output.
  *   workspace  spdp_adapt_grad_workspace bytes; the rest as for spdp_adapt.
  *
  * The sums over an adapter's tokens run in a fixed order: equal inputs give
@@ -408,9 +410,10 @@ typedef struct spdp_heads {
  *
  * spdp_rotate_heads_grad -- the gradients: y receives that with respect to x
  * (it may be its own x or dy as a whole), dweight that with respect to weight
- * (the sum over tokens and heads, in a fixed order). `workspace` is device
- * memory, 256-byte aligned, of spdp_rotate_heads_grad_workspace bytes (0
- * without weights), the call's alone until the stream has passed it.
+ * (the sum over tokens and heads, in a fixed order; it overlaps no other
+ * array). `workspace` is device memory, 256-byte aligned, of
+ * spdp_rotate_heads_grad_workspace bytes (0 without weights), the call's alone
+ * until the stream has passed it.
  */
 int spdp_rotate_heads(const spdp_heads_t* inputs, int32_t n_inputs,
                       const spdp_rotation_t* rotation, int64_t n_tokens,

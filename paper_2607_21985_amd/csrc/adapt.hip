@@ -921,8 +921,13 @@ int check_tokens(int64_t n_tokens) {
 
 bool overlap(const void* p, size_t np, const void* q, size_t nq) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + nq && b < a + np;
+  return p && q && a < b + nq && b < a + np;
 }
+
+struct Array {
+  const void* p;
+  size_t bytes;
+};
 
 // fp32 of the rank activations' partial sums
 size_t part_bytes(long long n_tokens, int rank, int splits) { return aligned((size_t)splits * n_tokens * rank * 4); }
@@ -1163,13 +1168,22 @@ int adapt(const spdp_adapters_t* banks, int32_t n_banks, const uint16_t* const* 
   for (int i = 0; i < n_banks; ++i) {
     if (!X[i] || !base[i] || !Y[i] || (H && !H[i])) return fail(SPDP_ERR_INVALID_ARG, "X, base, Y or H of a bank is NULL");
     const size_t out = n * banks[i].rows * 2, kept = n * banks[i].rank * 4;
+    if (overlap(Y[i], out, ids, n * 4) || (H && overlap(H[i], kept, ids, n * 4)))
+      return fail(SPDP_ERR_INVALID_ARG, "an output overlaps the ids");
     for (int j = 0; j < n_banks; ++j) {
-      const size_t in = n * banks[j].cols * 2, other = n * banks[j].rows * 2;
-      if (overlap(Y[i], out, X[j], in)) return fail(SPDP_ERR_INVALID_ARG, "an output overlaps an input");
+      const size_t fac = (size_t)banks[j].count * banks[j].rank, other = n * banks[j].rows * 2;
+      const Array in[] = {{X[j], n * banks[j].cols * 2},
+                          {banks[j].a, fac * banks[j].cols * 2},
+                          {banks[j].b, fac * banks[j].rows * 2},
+                          {banks[j].scale, (size_t)banks[j].count * 4}};
+      for (const Array& v : in) {
+        if (overlap(Y[i], out, v.p, v.bytes)) return fail(SPDP_ERR_INVALID_ARG, "an output overlaps an input");
+        if (H && overlap(H[i], kept, v.p, v.bytes)) return fail(SPDP_ERR_INVALID_ARG, "H overlaps another array");
+      }
       if (overlap(Y[i], out, base[j], other) && !(i == j && Y[i] == base[j]))
         return fail(SPDP_ERR_INVALID_ARG, "an output overlaps a base other than its own as a whole");
       if (i != j && overlap(Y[i], out, Y[j], other)) return fail(SPDP_ERR_INVALID_ARG, "outputs overlap");
-      if (H && (overlap(H[i], kept, X[j], in) || overlap(H[i], kept, base[j], other) || overlap(H[i], kept, Y[j], other) ||
+      if (H && (overlap(H[i], kept, base[j], other) || overlap(H[i], kept, Y[j], other) ||
                 (i != j && overlap(H[i], kept, H[j], kept))))
         return fail(SPDP_ERR_INVALID_ARG, "H overlaps another array");
     }
@@ -1229,17 +1243,15 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
   if (st != SPDP_OK) return st;
   if (!X || !H || !dY || !base || !dX || !dA || !dB) return fail(SPDP_ERR_INVALID_ARG, "an array is NULL");
   const size_t n = (size_t)n_tokens, fac = (size_t)bank->count * bank->rank;
-  const struct {
-    const void* p;
-    size_t bytes;
-  } in[] = {{X, n * bank->cols * 2}, {H, n * bank->rank * 4}, {dY, n * bank->rows * 2}, {base, n * bank->cols * 2},
-            {bank->a, fac * bank->cols * 2}, {bank->b, fac * bank->rows * 2}},
-    out[] = {{dX, n * bank->cols * 2}, {dA, fac * bank->cols * 4}, {dB, fac * bank->rows * 4}};
-  for (const auto& o : out) {
-    for (const auto& i : in)
+  const Array in[] = {{X, n * bank->cols * 2}, {H, n * bank->rank * 4}, {dY, n * bank->rows * 2}, {base, n * bank->cols * 2},
+                      {bank->a, fac * bank->cols * 2}, {bank->b, fac * bank->rows * 2}, {bank->scale, (size_t)bank->count * 4},
+                      {ids, n * 4}};
+  const Array out[] = {{dX, n * bank->cols * 2}, {dA, fac * bank->cols * 4}, {dB, fac * bank->rows * 4}};
+  for (const Array& o : out) {
+    for (const Array& i : in)
       if (overlap(o.p, o.bytes, i.p, i.bytes) && !(&o == &out[0] && &i == &in[3] && i.p == o.p))
         return fail(SPDP_ERR_INVALID_ARG, "an output overlaps an input (dX may be its base as a whole)");
-    for (const auto& q : out)
+    for (const Array& q : out)
       if (&q != &o && overlap(o.p, o.bytes, q.p, q.bytes)) return fail(SPDP_ERR_INVALID_ARG, "outputs overlap");
   }
   int cus = 1;

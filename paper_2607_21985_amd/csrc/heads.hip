@@ -471,8 +471,12 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
       if (i != j && overlap(in[i].y, n, in[j].y, other)) return fail(SPDP_ERR_INVALID_ARG, "outputs overlap");
       if (overlap(in[i].y, n, in[j].weight, (size_t)r->dim * 2)) return fail(SPDP_ERR_INVALID_ARG, "an output overlaps a weight");
     }
+    const size_t table = (size_t)r->table * r->rot * 2;
     if (back && in[i].dweight) {
       const size_t own = (size_t)r->dim * 4;
+      if (overlap(in[i].dweight, own, r->positions, (size_t)n_tokens * 4) || overlap(in[i].dweight, own, r->cosine, table) ||
+          overlap(in[i].dweight, own, r->sine, table))
+        return fail(SPDP_ERR_INVALID_ARG, "a weight's gradient overlaps the positions or the tables");
       for (int j = 0; j < inputs; ++j) {
         const size_t other = row * in[j].heads;
         if (overlap(in[i].dweight, own, in[j].x, other) || overlap(in[i].dweight, own, in[j].dy, other) ||
@@ -481,8 +485,8 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
           return fail(SPDP_ERR_INVALID_ARG, "a weight's gradient overlaps another array");
       }
     }
-    if (overlap(in[i].y, n, r->positions, (size_t)n_tokens * 4) ||
-        overlap(in[i].y, n, r->cosine, (size_t)r->table * r->rot * 2) || overlap(in[i].y, n, r->sine, (size_t)r->table * r->rot * 2))
+    if (overlap(in[i].y, n, r->positions, (size_t)n_tokens * 4) || overlap(in[i].y, n, r->cosine, table) ||
+        overlap(in[i].y, n, r->sine, table))
       return fail(SPDP_ERR_INVALID_ARG, "an output overlaps the positions or the tables");
   }
   int cus = 1;
