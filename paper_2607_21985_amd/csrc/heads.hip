@@ -206,11 +206,24 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
     const int tok = (int)(q / chunks);
     const int h0 = (int)(q % chunks) * chunk;
     const int pos = a.pos[tok];
-    const bool inside = (unsigned)pos < (unsigned)a.positions;
-    if (!BACK && !inside) continue;  // a padding token
+    if ((unsigned)pos >= (unsigned)a.positions) {  // a padding token
+      if constexpr (BACK) {
+        // (zeros as such: products with no numbers would not be where a weight is NaN)
+        const float zeros[V] = {};
+        for (int h = h0 + group; h < min(h0 + chunk, m.heads); h += groups) {
+          const size_t at = ((size_t)tok * m.heads + h) * a.dim;
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if (t[r].a < a.dim) store_v<V, ONCE>(m.y + at + t[r].a, zeros);
+            if (t[r].b < a.dim) store_v<V, ONCE>(m.y + at + t[r].b, zeros);
+          }
+        }
+      }
+      continue;
+    }
     Turn<V, PAIRS> u[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) u[r].load(a, t[r], inside ? pos : 0, BACK ? -1.0f : 1.0f);
+    for (int r = 0; r < R; ++r) u[r].load(a, t[r], pos, BACK ? -1.0f : 1.0f);
     // a head's numbers, requested a head ahead
     Raw<V> nx[R][2], ng[R][2];
     auto request = [&](int h) __attribute__((always_inline)) {
@@ -222,7 +235,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
           const int from = k == 0 ? t[r].a : t[r].b;
           nx[r][k].clear();
           if (BACK) ng[r][k].clear();
-          if (h < m.heads && inside && from < a.dim) {
+          if (h < m.heads && from < a.dim) {
             if (!BACK || norm) nx[r][k].template load<ONCE && BACK>(m.x + at + from);
             if (BACK) ng[r][k].template load<ONCE>(m.dy + at + from);
           }
@@ -260,8 +273,8 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(HeadsArgs a) {
         sum = head_sum(sum, a.lanes);
         if (BACK) dot = head_sum(dot, a.lanes);
       }
-      // (heads that are none, and padding, would divide by 0 where eps is 0)
-      const float rms = norm && on && inside ? 1.0f / __fsqrt_rn(sum * inv_dim + a.eps) : 1.0f;
+      // (heads that are none would divide by 0 where eps is 0)
+      const float rms = norm && on ? 1.0f / __fsqrt_rn(sum * inv_dim + a.eps) : 1.0f;
       const float back = rms * rms * (dot * inv_dim);
 #pragma unroll
       for (int r = 0; r < R; ++r) {

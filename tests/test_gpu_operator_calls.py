@@ -96,3 +96,29 @@ def test_results_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(got, want)
     m.close()
+
+
+@pytest.mark.parametrize("dim,rot", [(128, 128), (96, 32), (34, 6), (250, 126), (512, 512)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("where", ["table", "weight", "infinite weight"])
+def test_gradients_of_padding_are_0_beside_bad_numbers(dim, rot, interleaved, where):
+    # bad numbers that padding tokens have nothing to do with: the first position's
+    # angles, which no token has, or the weight
+    torch.manual_seed(dim + rot)
+    n, heads, table = 9, 3, 20
+    cos, sin = _tables(table, rot)
+    weight = (1 + 0.1 * torch.randn(dim, device="cuda")).half()
+    if where == "table":
+        cos[0], sin[0] = float("nan"), float("inf")
+    else:
+        weight[1] = float("nan") if where == "weight" else float("inf")
+    pos = torch.tensor([3, -1, 5, table, 1, 2 ** 31 - 1, -2 ** 31, 19, 1], device="cuda", dtype=torch.int32)
+    padding = (pos < 0) | (pos >= table)
+    x, dy = _half(n, heads * dim), _half(n, heads * dim)
+    x[padding], dy[padding] = float("nan"), float("inf")
+    for dx in (torch.full_like(x, 7.0), x.clone(), dy.clone()):
+        dw = torch.full((dim,), 7.0, device="cuda")
+        spdp.rotate_heads_grad([x], dim, pos, cos, sin, [dy], [dx], weights=[weight], dweights=[dw], interleaved=interleaved)
+        assert torch.equal(dx[padding], torch.zeros_like(dx[padding]))
+        assert torch.isfinite(dx[~padding]).all() == (where == "table")
+        assert torch.isfinite(dw).all()  # (the weight's gradient does not depend on the weight)
