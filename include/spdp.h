@@ -360,6 +360,11 @@ int spdp_adapt(const spdp_adapters_t* banks, int32_t n_banks,
  *              output.
  *   workspace  spdp_adapt_grad_workspace bytes; the rest as for spdp_adapt.
  *
+ * Sums are fp32. Where an adapter has more than 64 tokens, u and h meet x and
+ * dY as two fp16 numbers each, together exact to 2^-22 of a number or to 2^-37
+ * of the largest among the adapter's tokens; else as they are. An infinity in
+ * X or dY may make the entries of dA and dB that it meets NaN.
+ *
  * The sums over an adapter's tokens run in a fixed order: equal inputs give
  * equal bits.
  */

@@ -22,6 +22,8 @@
 // power of two, so that the largest lies in [2^13, 2^14), and split into the
 // nearest fp16 and the rest's nearest fp16: 22 bits or, for small ones, 2^-38
 // of the largest. Two MFMAs instead of one; the launches are bound by memory.
+// In the factors' gradients, which are fp32, the sums over up to kFew tokens take
+// fp32 MFMAs instead.
 //
 // Measured, on a card that copies at 5.2 TB/s: shrink_kernel, 2048 tokens, 8192
 // wide, rank 32, 11.2 us (34 MB of input, 3 TB/s, and the factor from L2);
@@ -455,7 +457,16 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
 // Outer: for an adapter, out[j][f] = scale * sum over its tokens of act[t][j]
 // in[t][f]. A piece is an adapter's tokens or, split, a part of them.
 //
-// With few tokens outer_kernel makes the operands itself (DIRECT), a launch less.
+// An adapter of up to kFew tokens: fp32 MFMAs on the activations as they are (lane l
+// has rank l mod 32 and the tokens 8 (l / 32) .. + 7, and of the input column l mod
+// 32 and the same tokens, so step e of eight multiplies tokens e and 8 + e). In sums
+// of so few products the 22 bits of two fp16 would show, and in ranks far below the
+// others fewer; in sums of more the additions' own error is as large. A product takes
+// the matrix cores eight times as long as those of the two fp16 (backward passes,
+// 4096 x 4096, two fp16 / fp32: 32 tokens of rank 16 18.2 / 18.8 us, 64 of four
+// adapters of rank 64 25.2 / 25.2, 2000 of 64 of rank 16 63.5 / 70).
+//
+// With few tokens in all outer_kernel makes the operands itself (DIRECT), a launch less.
 // Else pack_kernel lays a piece's activations out as the MFMA's operands, scaled by
 // one power of two (by each token's largest, which expand_kernel has left) and
 // split into two fp16: [group of 16 tokens][block of 32
@@ -464,7 +475,8 @@ __global__ __launch_bounds__(64 * (FUSED ? kFusedWaves : kWaves)) void expand_ke
 // through the wave's LDS and transposing reads, one group ahead, and the waves'
 // sums are added in LDS at the end.
 
-constexpr int kGroup = 16;  // tokens of an MFMA
+constexpr int kGroup = 16;  // tokens of an MFMA (of fp16)
+constexpr int kFew = 64;
 
 struct Piece {
   int t0, t1;        // in perm
@@ -517,6 +529,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
   const Outer& m = a.m[which];
   const Piece p = piece_of(a, adapter, blockIdx.y);
   const int n = p.t1 - p.t0;
+  if (n <= kFew) return;  // (what it would pack is not read)
   float up, down;
   piece_scale<kWaves>(a, m, p, all, up, down);
   if (threadIdx.x == 0 && blockIdx.x == 0) m.down[p.index] = down;
@@ -545,13 +558,20 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(OuterArgs a) {
   }
 }
 
+// The waves of a SIMD that the form of few tokens, which needs more registers, must
+// not cost the other.
+constexpr int outer_occupancy(int rb, int w, int fb, bool direct) {
+  return direct || w == 8 ? 1 : rb * fb == 8 ? 2 : rb == 2 ? 4 : 3;
+}
+
 template <int RB, int W, int FB, bool DIRECT>  // 32 RB ranks, W waves, 32 FB columns
-__global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
+__global__ __launch_bounds__(64 * W, outer_occupancy(RB, W, FB, DIRECT)) void outer_kernel(OuterArgs a) {
   constexpr int kRow = 64 * FB + 16;  // bytes of a token's columns in LDS, padded
   constexpr int kRowLanes = 4 * FB;   // lanes that load a token's columns
   constexpr int kRows = 64 / kRowLanes;
   constexpr int kRed = 4 * W * 2 * 16 * 64;
   constexpr int kIn = W * kGroup * kRow;
+  static_assert(kFew <= W * kGroup, "few tokens are one group a wave");
   __shared__ __attribute__((aligned(16))) unsigned char lds[kRed > kIn ? kRed : kIn];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -572,8 +592,11 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
   const half8* const packed = reinterpret_cast<const half8*>(m.packed) + piece.group0 * RB * 128 + lane;
   const int groups = (piece.t1 - piece.t0 + kGroup - 1) / kGroup;
   const half8 none = half8{0, 0, 0, 0, 0, 0, 0, 0};
+  const bool few = piece.t1 - piece.t0 <= kFew;
   float up = 1.0f, down = 1.0f;
-  if constexpr (DIRECT) piece_scale<W>(a, m, piece, reinterpret_cast<float*>(lds), up, down);
+  if constexpr (DIRECT) {
+    if (!few) piece_scale<W>(a, m, piece, reinterpret_cast<float*>(lds), up, down);
+  }
 
   // a group's input and operands, requested a group ahead, its tokens' places
   // two ahead
@@ -587,7 +610,7 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
       at[p] = t < piece.t1 ? (a.perm ? a.perm[t] : t) : -1;
     }
   };
-  auto request = [&](int g) __attribute__((always_inline)) {
+  auto request_in = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int p = 0; p < FB; ++p) in[p] = none;
     if (!DIRECT && m.stream) {
@@ -599,19 +622,60 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
       for (int p = 0; p < FB; ++p)
         if (at[p] >= 0 && left > 0) in[p] = load8_inside(m.in + (size_t)at[p] * m.width + col, left);
     }
+  };
+  auto keep_in = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < FB; ++p)
+      *reinterpret_cast<half8*>(mine + (kRows * p + lane / kRowLanes) * kRow + 16 * (lane % kRowLanes)) = in[p];
+  };
+  // the activations of ranks 32 j + lane mod 32 and of the lane's eight tokens
+  auto load_raw = [&](int g, auto& to) __attribute__((always_inline)) {
+    int from[8];
+    rows_of(a, piece.t0 + g * kGroup + 8 * (lane >> 5), piece.t1, from);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < RB; ++j) {
+        const uint32_t bytes = 4u * ((uint32_t)from[e] * (uint32_t)a.rank + (uint32_t)min(32 * j + (lane & 31), a.rank - 1));
+        to[j][e] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(m.act) + bytes);
+      }
+  };
+  auto there = [&](int g, int j, int e) __attribute__((always_inline)) {
+    return piece.t0 + g * kGroup + 8 * (lane >> 5) + e < piece.t1 && 32 * j + (lane & 31) < a.rank;
+  };
+  auto request = [&](int g) __attribute__((always_inline)) {
+    request_in();
     if constexpr (DIRECT) {
-      int from[8];
-      rows_of(a, piece.t0 + g * kGroup + 8 * (lane >> 5), piece.t1, from);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int j = 0; j < RB; ++j) raw[j][e] = m.act[(uint32_t)from[e] * (uint32_t)a.rank + (uint32_t)min(32 * j + (lane & 31), a.rank - 1)];
+      load_raw(g, raw);
     } else {
 #pragma unroll
       for (int j = 0; j < 2 * RB; ++j) act[j] = packed[(size_t)g * RB * 128 + 64 * j];
     }
   };
   int g = wave;
+  if (few && g < groups) {
+    float x[RB][8];
+    places(g);
+    request_in();
+    load_raw(g, x);
+    keep_in();
+    wave_fence();
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[j][e] = there(g, j, e) ? x[j][e] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < FB; ++i) {
+      const half8 v = read_transposed(mine, kRow, 0, 32 * i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+#pragma unroll
+        for (int j = 0; j < RB; ++j) acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j][e], (float)v[e], acc[j][i], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  if (few) g = groups;
   if (g < groups) {
     places(g);
     request(g);
@@ -619,17 +683,14 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
   }
   for (; g < groups; g += W) {
     half8 now[2 * RB];
-#pragma unroll
-    for (int p = 0; p < FB; ++p)
-      *reinterpret_cast<half8*>(mine + (kRows * p + lane / kRowLanes) * kRow + 16 * (lane % kRowLanes)) = in[p];
+    keep_in();
     if constexpr (DIRECT) {
 #pragma unroll
       for (int j = 0; j < RB; ++j)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           _Float16 hi, lo;
-          const bool there = piece.t0 + g * kGroup + 8 * (lane >> 5) + e < piece.t1 && 32 * j + (lane & 31) < a.rank;
-          split2(there ? raw[j][e] * up : 0.0f, hi, lo);
+          split2(there(g, j, e) ? raw[j][e] * up : 0.0f, hi, lo);
           now[2 * j][e] = hi;
           now[2 * j + 1][e] = lo;
         }
@@ -654,7 +715,7 @@ __global__ __launch_bounds__(64 * W) void outer_kernel(OuterArgs a) {
     wave_fence();
   }
 
-  if constexpr (!DIRECT) down = m.down[piece.index];
+  if constexpr (!DIRECT) down = few ? 1.0f : m.down[piece.index];
   const float by = down * a.scale[adapter];
   float* const red = reinterpret_cast<float*>(lds);  // [wave][two column blocks][register][lane]
   float* const out = m.out + ((size_t)blockIdx.y * a.count + adapter) * a.rank * m.width;

@@ -122,3 +122,48 @@ def test_gradients_of_padding_are_0_beside_bad_numbers(dim, rot, interleaved, wh
         assert torch.equal(dx[padding], torch.zeros_like(dx[padding]))
         assert torch.isfinite(dx[~padding]).all() == (where == "table")
         assert torch.isfinite(dw).all()  # (the weight's gradient does not depend on the weight)
+
+
+@pytest.mark.parametrize("n,count,rank,how", [
+    (1, 1, 1, "one"), (1, 1, 24, "one"), (4, 1, 16, "one"), (64, 1, 33, "one"), (30, 4, 24, "mixed"), (200, 12, 8, "mixed"),
+    (64, 1, 128, "one"), (16, 2, 64, "mixed"),
+    (600, 40, 24, "mixed"), (700, 20, 40, "mixed"), (540, 64, 128, "mixed"), (3000, 3, 20, "few")])
+def test_gradients_of_few_tokens_have_the_bits_of_fp32(n, count, rank, how):
+    # ranks whose activations lie far below one another: each has the error of fp32
+    # products and sums in any order (2 2^-24 of the magnitudes for each addition: the
+    # tokens, the waves and the scale), whatever the others' size. (3000 tokens: one
+    # adapter has almost all, the others have few.)
+    rows, cols, u32 = 264, 520, 2.0 ** -24
+    rng = np.random.default_rng(n + rank)
+    sizes = 2.0 ** -rng.permutation(np.linspace(0, 24, rank).astype(int)) if rank > 1 else np.ones(1)
+    ids = np.zeros(n, dtype=np.int32) if how == "one" else rng.integers(-1, count, n).astype(np.int32)
+    if how == "few":
+        ids[:] = np.where(rng.random(n) < 0.01, rng.integers(1, count, n), 0)
+    a = rng.normal(size=(count, rank, cols)).astype(np.float16)
+    b = (rng.normal(size=(count, rank, rows)) * sizes[None, :, None]).astype(np.float16)
+    b[:, :, 2:] = 0  # u is a sum of two products, so that its own error is small
+    scale = np.exp(rng.normal(size=count)).astype(np.float32)
+    x, dy = rng.normal(size=(n, cols)).astype(np.float16), rng.normal(size=(n, rows)).astype(np.float16)
+    h = (rng.normal(size=(n, rank)) * sizes).astype(np.float32)
+    dev = lambda v: torch.from_numpy(v).cuda()  # noqa: E731
+    bank = spdp.Adapters(dev(a), dev(b), dev(scale))
+    dx, da, db = torch.empty(n, cols, dtype=torch.float16, device="cuda"), torch.empty(a.shape, device="cuda"), \
+        torch.empty(b.shape, device="cuda")
+    bank.grad_into(dev(x), None if how == "one" else dev(ids), dev(h), dev(dy), torch.zeros_like(dx), dx, da, db)
+    few = 0
+    for i in range(count):
+        at = np.flatnonzero(ids == i)
+        k = at.size
+        if k == 0 or k > 64:
+            continue
+        few += 1
+        front, b2 = dy[at, :2].astype(np.float64), b[i, :, :2].astype(np.float64).T
+        # (the matrix cores align the products of a subnormal fp16 as those of 2^-14)
+        u, u_err = front @ b2, 4 * u32 * (np.abs(front) @ np.maximum(np.abs(b2), 2.0 ** -14))
+        for got, act, own, z in ((da[i], u, u_err, x[at]), (db[i], h[at].astype(np.float64), np.zeros_like(u), dy[at])):
+            z, s = z.astype(np.float64), float(scale[i])
+            want, size = s * (act.T @ z), s * ((np.abs(act) + own).T @ np.abs(z))
+            bound = s * (own.T @ np.abs(z)) + 2 * (k + 10) * u32 * size
+            err = np.abs(got.cpu().numpy().astype(np.float64) - want)
+            assert np.all(err <= bound), (i, k, np.max(err / np.maximum(size, 1e-300)))
+    assert few
