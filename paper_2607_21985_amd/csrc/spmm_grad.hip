@@ -470,7 +470,8 @@ float model_us(const spdp_matrix* h, const Form& f, long long wgs, int per, int 
 
 // The form and split of the least modelled time, within 256 MB of partial sums.
 // SPDP_GRAD_FORM (a testing aid) forces a form by its place in the table, or the
-// plain one (-1), SPDP_GRAD_SPLITS the ranges.
+// plain one (-1, and where the forced one's LDS does not fit), SPDP_GRAD_SPLITS the
+// ranges.
 void plan_grad(const spdp_matrix* h, long long n_tokens, GradPlan* p) {
   const int cus = std::max(1, h->cus);
   const int forced_splits = env_int("SPDP_GRAD_SPLITS", 0), forced_form = env_int("SPDP_GRAD_FORM", -2);

@@ -52,3 +52,69 @@ out["statuses"] = [adapt(y=[A + 4 * 8 * 128 * 2]), adapt(y=[A - y]), adapt(y=[S4
                    rotate_grad([one(dy=Y, w=1 << 35, dw=(1 << 36) + 64)])]
 """]))
     assert out["statuses"] == [0] * 13
+
+
+# rows, cols, share of the values that are kept, tokens; and the form (blocks of 32
+# tokens of a wave, groups of 32 columns, groups of tokens) that the calls take by
+# themselves on 256 compute units
+GRAD_DEFAULTS = [
+    (1000, 2056, 0.2, 70, (1, 4, 1)),
+    (1003, 1280, 0.2, 1000, (2, 4, 1)),
+    (2048, 2048, 0.5, 700, (4, 4, 2)),
+    (1536, 6144, 0.25, 16, (1, 8, 1)),
+    (2051, 8192, 0.25, 70, (1, 8, 1)),
+    (2048, 2048, 0.5, 200, (2, 8, 1)),
+    (2051, 8192, 0.25, 500, (2, 8, 1)),
+    (1536, 6144, 0.25, 100, (4, 8, 1)),
+    (2051, 8192, 0.25, 300, (4, 8, 1)),
+    (1536, 6144, 0.25, 1500, (8, 8, 1)),
+    (2051, 8192, 0.25, 1500, (8, 8, 1)),
+]
+# the forms by their place in the table, and matrices sparse enough for each (with rows
+# that are 16-byte aligned and rows that are not, the last columns a part of a workgroup's)
+GRAD_FORMS = [(1, 4, 1), (2, 4, 1), (4, 4, 1), (4, 4, 2), (1, 8, 1), (2, 8, 1), (4, 8, 1), (8, 8, 1)]
+GRAD_SPARSE = [(1000, 1016, 0.2), (803, 616, 0.25), (2056, 328, 0.3)]
+
+GRAD = """
+def form(m, n):
+    s = S()
+    assert L.spdp_spmm_grad_workspace(m._h, n, ctypes.byref(s)) == 0
+    log()
+    assert L.spdp_spmm_grad(m._h, X, n, Y, WS, s.value, None) == 0
+    name = launches()[0][0]
+    found = re.match(r"grad_kernelILi(\\d+)ELi(\\d+)ELi(\\d+)ELb(\\d)E", name)
+    return [int(v) for v in found.groups()] if found else name
+"""
+
+
+def test_the_gradients_forms_by_default(fake_hip):  # noqa: F811
+    out = run(fake_hip, "\n".join([BODY, GRAD, f"""
+hip.fake_cus(256)
+out["got"] = []
+for rows, cols, keep, n, _ in {GRAD_DEFAULTS}:
+    m = ones(rows, cols, (256, 16), keep)
+    out["got"].append(form(m, n))
+    m.close()
+"""]))
+    assert out["got"] == [[*f, int(rows % 8 == 0)] for rows, _, _, _, f in GRAD_DEFAULTS]
+
+
+@pytest.mark.parametrize("place", range(len(GRAD_FORMS)))
+def test_a_forced_form_of_the_gradient_is_the_one_that_runs(fake_hip, place):  # noqa: F811
+    out = run(fake_hip, "\n".join([BODY, GRAD, f"""
+hip.fake_cus(256)
+out["got"] = []
+for rows, cols, keep in {GRAD_SPARSE}:
+    m = ones(rows, cols, (256, 16), keep)
+    out["got"] += [form(m, n) for n in (1, 300, 700)]
+    m.close()
+"""]), env={"SPDP_GRAD_FORM": str(place)})
+    assert out["got"] == [[*GRAD_FORMS[place], int(rows % 8 == 0)] for rows, _, _ in GRAD_SPARSE for _ in range(3)]
+
+
+def test_a_forced_form_that_does_not_fit_is_the_plain_one(fake_hip):  # noqa: F811
+    # 256 tokens and 256 columns of a dense matrix: 64 KB of dY and 256 of values
+    out = run(fake_hip, "\n".join([BODY, GRAD, """
+out["got"] = form(ones(512, 512, (256, 16)), 600)
+"""]), env={"SPDP_GRAD_FORM": "7"})
+    assert out["got"].startswith("grad_plain")
