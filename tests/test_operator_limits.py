@@ -118,3 +118,46 @@ def test_a_forced_form_that_does_not_fit_is_the_plain_one(fake_hip):  # noqa: F8
 out["got"] = form(ones(512, 512, (256, 16)), 600)
 """]), env={"SPDP_GRAD_FORM": "7"})
     assert out["got"].startswith("grad_plain")
+
+
+def test_the_workspace_asked_for_suffices_and_less_is_refused(fake_hip):  # noqa: F811
+    out = run(fake_hip, "\n".join([BODY, """
+hip.fake_cus(256)
+out["wrong"], out["asked"] = [], 0
+def check(label, size, call):
+    enough = call(size)
+    less = call(size - 1) if size else -1
+    out["asked"] += size > 0
+    if enough != 0 or less != -1:
+        out["wrong"].append([label, size, enough, less])
+sizes = (1, 31, 64, 65, 512, 513, 1000, 5000, 1 << 20)
+for n in sizes:
+    for rank in (1, 17, 40, 128):
+        for count in (1, 64, 2048):
+            for ids in (None, IDS):
+                for wide in (1, 16):
+                    m = bank(rows=256 * wide, cols=128 * wide, rank=rank, count=count)
+                    label = [n, rank, count, bool(ids), wide]
+                    for k in (1, 3):
+                        check(label + ["adapt", k], need([m] * k, n, ids is not None)[1],
+                              lambda room: adapt([m] * k, n=n, ids=ids, room=room, x=[X] * k,
+                                                 base=[BASE + (i << 38) for i in range(k)], y=[OUT + (i << 38) for i in range(k)]))
+                    s = S()
+                    assert L.spdp_adapt_grad_workspace(ctypes.byref(m), n, ids is not None, ctypes.byref(s)) == 0
+                    check(label + ["grad"], s.value, lambda room: grad(m, n=n, ids=ids, room=room))
+for n in sizes:
+    for dim, rot in ((128, 128), (512, 2), (34, 6)):
+        for k in (1, 2):
+            ms = [one(x=X + (i << 40), dy=Y + (i << 42), y=OUT + (i << 41), w=1 << 35, dw=(1 << 34) + 4096 * i, n=1 + 7 * i)
+                  for i in range(k)]
+            s, r = S(), rotation(dim=dim, rot=rot)
+            assert L.spdp_rotate_heads_grad_workspace(heads(*ms), k, ctypes.byref(r), n, ctypes.byref(s)) == 0
+            check([n, dim, rot, k], s.value, lambda room: rotate_grad(ms, r, n, room=room))
+m = ones(1000, 328, (256, 16), 0.5)
+for n in (1, 90, 700, 5000):
+    s = S()
+    assert L.spdp_spmm_grad_workspace(m._h, n, ctypes.byref(s)) == 0
+    check([n, "pruned"], s.value, lambda room: L.spdp_spmm_grad(m._h, X, n, Y, WS, room, None))
+"""]))
+    assert not out["wrong"], out["wrong"][:5]
+    assert out["asked"] > 500
