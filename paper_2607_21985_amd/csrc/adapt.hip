@@ -38,7 +38,7 @@
 #include <algorithm>
 #include <cstring>
 
-#include "internal.h"
+#include "calls.h"
 #include "lanes.h"
 #include "lowrank.h"
 
@@ -866,25 +866,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int* ids, int 
 // ---------------------------------------------------------------------------
 // Host side.
 
-using spdp::fail;
-
-int hip_fail(hipError_t e, const char* what) {
-  return fail(SPDP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
+using namespace spdp;
 
 constexpr int kLdsPlain = 48 * 1024;  // dynamic LDS that a launch may have without asking
-
-size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
-
-int compute_units(int* cus) {
-  int dev = -1;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-  e = hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
-  if (e != hipSuccess) return hip_fail(e, "hipDeviceGetAttribute");
-  *cus = std::max(1, *cus);
-  return SPDP_OK;
-}
 
 // The ranges of the width that shrink_kernel's workgroups take: one workgroup
 // per CU, at least four steps each (one per wave), at most eight ranges, for
@@ -979,16 +963,6 @@ int check_tokens(int64_t n_tokens) {
   if (n_tokens > 1 << 20) return fail(SPDP_ERR_UNSUPPORTED, "more than 2^20 tokens");
   return SPDP_OK;
 }
-
-bool overlap(const void* p, size_t np, const void* q, size_t nq) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && a < b + nq && b < a + np;
-}
-
-struct Array {
-  const void* p;
-  size_t bytes;
-};
 
 // fp32 of the rank activations' partial sums
 size_t part_bytes(long long n_tokens, int rank, int splits) { return aligned((size_t)splits * n_tokens * rank * 4); }
@@ -1199,15 +1173,6 @@ void plan_grad(const spdp_adapters_t* m, long long n_tokens, bool ids, int cus, 
   p->bytes = p->sort.bytes + p->part + p->u + p->outer[0] + p->outer[1] + 2 * (p->packed + p->down) + p->most;
 }
 
-int check_workspace(const void* workspace, size_t have, size_t need) {
-  if (need == 0) return SPDP_OK;
-  if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
-  if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(SPDP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  if (have < need)
-    return fail(SPDP_ERR_INVALID_ARG, "workspace of " + std::to_string(have) + " bytes, " + std::to_string(need) + " needed");
-  return SPDP_OK;
-}
-
 int adapt_workspace(const spdp_adapters_t* banks, int32_t n_banks, int64_t n_tokens, int32_t with_ids, size_t* bytes) {
   int st = check_banks(banks, n_banks, n_tokens);
   int cus = 1;
@@ -1383,17 +1348,6 @@ int adapt_grad(const spdp_adapters_t* bank, const uint16_t* X, const int32_t* id
     e = hipGetLastError();
   }
   return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");
-}
-
-// No C++ exception leaves the ABI: a message may find no memory.
-template <class F>
-int guarded(F f) {
-  try {
-    spdp::clear_error();
-    return f();
-  } catch (...) {
-    return SPDP_ERR_OOM;
-  }
 }
 
 }  // namespace

@@ -20,7 +20,7 @@
 #include <algorithm>
 #include <cstring>
 
-#include "internal.h"
+#include "calls.h"
 
 namespace {
 
@@ -354,11 +354,7 @@ __global__ __launch_bounds__(1024) void heads_sum_kernel(SumArgs a) {
   }
 }
 
-using spdp::fail;
-
-int hip_fail(hipError_t e, const char* what) {
-  return fail(SPDP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
+using namespace spdp;
 
 // The numbers that a lane reads at once, and the lanes and workgroups that
 // follow: 16 bytes where the pairs and heads divide into such vectors, else
@@ -408,8 +404,6 @@ void plan_heads(const spdp_heads_t* in, int inputs, const spdp_rotation_t* r, lo
   }
 }
 
-size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
-
 int check(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int64_t n_tokens) {
   if (!in || !r) return fail(SPDP_ERR_INVALID_ARG, "inputs or rotation is NULL");
   if (inputs < 1 || inputs > kMaxInputs) return fail(SPDP_ERR_INVALID_ARG, "the number of inputs must lie in [1, 8]");
@@ -440,21 +434,6 @@ void launch_pairs(const HeadsArgs& a, bool pairs, bool back, dim3 grid, hipStrea
   if constexpr (V > 1)
     if (pairs) return launch<V, R, true, ONCE>(a, back, grid, s);
   launch<V, R, false, ONCE>(a, back, grid, s);
-}
-
-int compute_units(int* cus) {
-  int dev = -1;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-  e = hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
-  if (e != hipSuccess) return hip_fail(e, "hipDeviceGetAttribute");
-  *cus = std::max(1, *cus);
-  return SPDP_OK;
-}
-
-bool overlap(const void* p, size_t np, const void* q, size_t nq) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && a < b + nq && b < a + np;
 }
 
 size_t grad_bytes(const spdp_heads_t* in, int inputs, int dim, const HeadsPlan& p) {
@@ -514,14 +493,8 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
   sum.dim = r->dim;
   int sums = 0;
   if (back) {
-    const size_t need = grad_bytes(in, inputs, r->dim, p);
-    if (need > 0) {
-      if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
-      if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(SPDP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-      if (workspace_bytes < need)
-        return fail(SPDP_ERR_INVALID_ARG,
-                    "workspace of " + std::to_string(workspace_bytes) + " bytes, " + std::to_string(need) + " needed");
-    }
+    st = check_workspace(workspace, workspace_bytes, grad_bytes(in, inputs, r->dim, p));
+    if (st != SPDP_OK) return st;
   }
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   size_t bytes = 0;
@@ -571,16 +544,6 @@ int heads(const spdp_heads_t* in, int32_t inputs, const spdp_rotation_t* r, int6
     e = hipGetLastError();
   }
   return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");
-}
-
-template <class F>
-int guarded(F f) {
-  try {
-    spdp::clear_error();
-    return f();
-  } catch (...) {  // a message found no memory
-    return SPDP_ERR_OOM;
-  }
 }
 
 }  // namespace

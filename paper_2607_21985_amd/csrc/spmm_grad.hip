@@ -21,7 +21,7 @@
 #include <cstdlib>
 #include <cstring>
 
-#include "internal.h"
+#include "calls.h"
 #include "lanes.h"
 
 namespace {
@@ -417,11 +417,7 @@ __global__ __launch_bounds__(kThreads) void grad_reduce_kernel(const float* __re
 // ---------------------------------------------------------------------------
 // Host side.
 
-using spdp::fail;
-
-int hip_fail(hipError_t e, const char* what) {
-  return fail(SPDP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
+using namespace spdp;
 
 constexpr int kLdsMax = 160 * 1024;
 
@@ -544,28 +540,21 @@ int check(const spdp_matrix* h, int64_t n_tokens) {
 
 int spmm_grad(spdp_handle_t h, const uint16_t* dY, int64_t n_tokens, uint16_t* dX, void* workspace, size_t workspace_bytes,
               void* stream) {
-  const int st = check(h, n_tokens);
+  int st = check(h, n_tokens);
   if (st != SPDP_OK) return st;
   if (!dY || !dX) return fail(SPDP_ERR_INVALID_ARG, "dY or dX is NULL");
   if ((reinterpret_cast<uintptr_t>(dY) | reinterpret_cast<uintptr_t>(dX)) & 15)
     return fail(SPDP_ERR_INVALID_ARG, "dY and dX must be 16-byte aligned");
-  const uintptr_t y0 = reinterpret_cast<uintptr_t>(dY), y1 = y0 + (uintptr_t)n_tokens * h->rows * 2;
-  const uintptr_t x0 = reinterpret_cast<uintptr_t>(dX), x1 = x0 + (uintptr_t)n_tokens * h->cols * 2;
-  if (x0 < y1 && y0 < x1) return fail(SPDP_ERR_INVALID_ARG, "dY and dX overlap");
+  if (overlap(dY, (size_t)n_tokens * h->rows * 2, dX, (size_t)n_tokens * h->cols * 2))
+    return fail(SPDP_ERR_INVALID_ARG, "dY and dX overlap");
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
   if (dev != h->device) return fail(SPDP_ERR_INVALID_ARG, "current device differs from the handle's");
   GradPlan p;
   plan_grad(h, n_tokens, &p);
-  const size_t need = part_bytes(h, n_tokens, p);
-  if (need > 0) {
-    if (!workspace) return fail(SPDP_ERR_INVALID_ARG, "workspace is NULL");
-    if (reinterpret_cast<uintptr_t>(workspace) & 255) return fail(SPDP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    if (workspace_bytes < need)
-      return fail(SPDP_ERR_INVALID_ARG,
-                  "workspace of " + std::to_string(workspace_bytes) + " bytes, " + std::to_string(need) + " needed");
-  }
+  st = check_workspace(workspace, workspace_bytes, part_bytes(h, n_tokens, p));
+  if (st != SPDP_OK) return st;
   GradArgs a;
   std::memset(&a, 0, sizeof(a));
   a.tile_offset = static_cast<const uint32_t*>(h->d_tile_offset);
@@ -605,16 +594,6 @@ int spmm_grad(spdp_handle_t h, const uint16_t* dY, int64_t n_tokens, uint16_t* d
     e = hipGetLastError();
   }
   return e == hipSuccess ? SPDP_OK : hip_fail(e, "kernel launch");
-}
-
-template <class F>
-int guarded(F f) {
-  try {
-    spdp::clear_error();
-    return f();
-  } catch (...) {  // a message found no memory
-    return SPDP_ERR_OOM;
-  }
 }
 
 }  // namespace
