@@ -382,7 +382,8 @@ class Matrix:
 
     def spmm_grad_into(self, dy, dx, stream=None) -> None:
         """Enqueue the gradient of ``spmm`` with respect to its input,
-        ``dx = dy W_sp``, for ``dy`` [tokens, rows] into ``dx`` [tokens, cols]."""
+        ``dx = dy W_sp``, for ``dy`` [tokens, rows] into ``dx`` [tokens, cols].
+        (torch's autograd does not know of it: ``spmm``'s result has no graph.)"""
         import torch
         n = dy.shape[0]
         _tensor(dy, "dy", torch.float16, (n, self.rows))
@@ -513,6 +514,9 @@ class Adapters:
 
     with the adapter ``id`` of each token. ``base`` is the shared projection's
     output (``Matrix``, ``spmspv_many``, ``Matrix.spmm``).
+
+    torch's autograd records none of the calls: a result has no graph, whether or
+    not its inputs require gradients, and the gradients are ``grad_into``'s.
     """
 
     def __init__(self, a, b, scale):
@@ -690,7 +694,8 @@ def rotate_heads(xs, dim, pos, cos, sin, ys, weights=None, eps=1e-6, interleaved
     rot / 2]; a token whose position is none of them is padding, and its outputs
     are left as they were. ``weights``: per input the norm's fp16 [dim] weight,
     or None for no norm. ``interleaved``: pairs are neighbours, else (i, i +
-    rot / 2)."""
+    rot / 2). torch's autograd does not record it: the gradients are
+    ``rotate_heads_grad``'s."""
     inputs, k, r, n, s = _heads(xs, dim, pos, cos, sin, ys, weights, eps, interleaved, stream)
     _check(lib().spdp_rotate_heads(inputs, k, r, n, s))
 

@@ -28,7 +28,7 @@
 // Measured, on a card that copies at 5.2 TB/s: shrink_kernel, 2048 tokens, 8192
 // wide, rank 32, 11.2 us (34 MB of input, 3 TB/s, and the factor from L2);
 // expand_kernel behind it, 28672 wide, 54 us (235 MB, 4.4 TB/s); outer_kernel, 4096
-// tokens, 13824 + 5120 wide, rank 64, 42 us (155 MB, 3.7 TB/s); sort_kernel, 2048
+// tokens, 13824 + 5120 wide, rank 64, 41 us (155 MB, 3.8 TB/s); sort_kernel, 2048
 // ids, 6 us, a chain of LDS round trips. Small calls are bound by the launches,
 // 4 to 7 us each.
 
@@ -888,8 +888,8 @@ Ranges shrink_ranges(int64_t width, long long tiles, int banks, int cus) {
 
 // The workgroups of outer_kernel without a split, the pieces that an adapter's
 // tokens are split into, and the waves of a workgroup: pieces of many tokens, four
-// workgroups per CU (of three that a CU holds); unsplit, eight waves where there
-// are fewer than two workgroups per CU. Whole backward passes, us, unsplit of
+// workgroups per CU (a CU holds five, four or two at up to 32, 64 and 128 ranks);
+// unsplit, eight waves where there are fewer than two workgroups per CU. Whole backward passes, us, unsplit of
 // four waves / of eight / split: 4096 tokens, 13824 x 5120, rank 64 143 / 144 /
 // 129; 2048, 4096 x 11008, rank 16 62 / 53 / 54; 4000 of 8 adapters, 8192 x 8192,
 // rank 8 107 / 111 / 108.

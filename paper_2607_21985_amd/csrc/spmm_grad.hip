@@ -9,10 +9,12 @@
 //     the kernel);
 //   * grad_plain_kernel, for the others.
 //
-// Measured, 13824 x 5120 at 70 % sparsity, 2048 tokens: 325 us, 890 TFLOP/s of the
-// dense product that the matrix cores execute; they are busy half of the cycles,
-// LDS and vector issue nearly as long, and the power limit holds the clock. 4096 x
-// 4096 at 50 %, 256 tokens: 26 us, bound by vector issue and the second launch.
+// Measured (whole calls among others), 13824 x 5120 at 70 % sparsity, 2048 tokens:
+// 324 to 331 us, 890 TFLOP/s of the dense product that the matrix cores execute; they
+// are busy half of the cycles, LDS and vector issue nearly as long, and the power
+// limit holds the clock (283 us on a dY of zeros; under a tracer 346 to 374 and 26 for
+// the second launch). 4096 x 4096 at 50 %, 256 tokens: 26 us, bound by vector issue
+// and the second launch.
 
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
