@@ -141,7 +141,8 @@ for n in sizes:
                     for k in (1, 3):
                         check(label + ["adapt", k], need([m] * k, n, ids is not None)[1],
                               lambda room: adapt([m] * k, n=n, ids=ids, room=room, x=[X] * k,
-                                                 base=[BASE + (i << 38) for i in range(k)], y=[OUT + (i << 38) for i in range(k)]))
+                                                 base=[BASE + (i << 38) for i in range(k)],
+                                                 y=[OUT + (i << 38) for i in range(k)]))
                     s = S()
                     assert L.spdp_adapt_grad_workspace(ctypes.byref(m), n, ids is not None, ctypes.byref(s)) == 0
                     check(label + ["grad"], s.value, lambda room: grad(m, n=n, ids=ids, room=room))
