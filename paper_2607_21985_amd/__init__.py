@@ -209,19 +209,27 @@ def _tensor(t, name: str, dtype, shape) -> None:
         raise ValueError(f"{name} must be a contiguous {list(shape)} tensor")
 
 
+_raw_stream = None  # a device's current stream
+
+
 def _stream(stream, tensors) -> int:
     """The HIP stream to enqueue on, after a check of the tensors' device."""
+    global _raw_stream
     import torch
     dev = tensors[0].get_device()  # -1: not on a GPU
     for t in tensors:
-        if t.get_device() != dev or dev < 0:
-            raise ValueError("all tensors must be on one GPU")
+        if t.get_device() != dev:
+            dev = -1
+    if dev < 0:
+        raise ValueError("all tensors must be on one GPU")
     if torch.cuda.current_device() != dev:
         raise ValueError("the tensors are not on the current device")
     if stream is None:
-        # (the stream's number alone: an object of it takes longer than a launch)
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
+        if _raw_stream is None:
+            # (the stream's number alone: an object of it takes longer than a launch)
+            _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+                (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        return _raw_stream(dev)
     if stream.device.index != dev:
         raise ValueError("the stream is not on the tensors' device")
     return stream.cuda_stream
@@ -607,15 +615,19 @@ def adapters_many(banks, xs, ids, bases, ys, hs=None, stream=None) -> None:
         raise ValueError("banks, xs, bases, ys and hs must have one entry per projection")
     f16, n, L = torch.float16, xs[0].shape[0], lib()
     some = [*xs, *bases, *ys]
-    bk, key = [], [n, ids is not None]
+    bk, key, seen, cols = [], [n, ids is not None], None, 0
     for m, x, base, y in zip(banks, xs, bases, ys):
         bk.append(m._struct())
         some.append(m.a)
         key.append(m._key)
-        _tensor(x, "x", f16, (n, m.cols))
+        if x is not seen or m.cols != cols:  # (mostly one input for all)
+            seen, cols = x, m.cols
+            _tensor(x, "x", f16, (n, cols))
         out = (n, m.rows)
-        _tensor(base, "base", f16, out)
-        _tensor(y, "y", f16, out)
+        if not (base.dtype is f16 and y.dtype is f16 and base.shape == out and y.shape == out and base.is_contiguous()
+                and y.is_contiguous()):
+            _tensor(base, "base", f16, out)
+            _tensor(y, "y", f16, out)
     if hs is not None:
         for m, h in zip(banks, hs):
             _tensor(h, "h", torch.float32, (n, m.rank))
